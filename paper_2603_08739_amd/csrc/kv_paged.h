@@ -1,0 +1,101 @@
+// kv_paged.h - internal declarations of the paged-cache operators (the public
+// contract is include/kvpaged.h).
+#pragma once
+
+#include "../../include/kvpaged.h"
+#include "kv_internal.h"
+
+namespace kv {
+
+// ---------------------------------------------------------------------------
+// work list of the attention (kv_paged_plan writes it, kv_paged_attention
+// walks it)
+// ---------------------------------------------------------------------------
+// The query rows of a request under one key/value head are its new tokens times
+// the G query heads that read the head, token by token (row = token * G +
+// head).  A tile is up to `rows` of them; a piece is a tile over a range of
+// keys.  Long tiles are cut into pieces so that the chip is filled and no
+// workgroup runs much longer than the others; the pieces of one tile are
+// joined by a second kernel.
+constexpr uint32_t kKeyUnit = 64;  // key ranges of pieces are cut at multiples of this
+
+struct PieceItem {
+  int32_t req;        // table row
+  int32_t q_start;    // the request's first token
+  int32_t ctx;        // tokens cached before them
+  int32_t row_end;    // rows of the request: new tokens * G
+  int32_t row0;       // the tile's first row
+  int32_t key_begin;  // multiple of kKeyUnit
+  int32_t key_end;
+  int32_t part;       // partial result to write, or -1: the tile's only piece
+};
+
+struct SplitTile {
+  int32_t q_start, row_end, row0;
+  int32_t first_part, n_parts;
+  int32_t pad[3];
+};
+
+struct WorkHeader {
+  int32_t n_items, n_split;
+  int32_t pad[62];
+};
+
+struct WorkLayout {
+  uint32_t rows;       // rows of a tile: 16, 32 or 64 (one tile a request) or 128
+  uint32_t group;      // G
+  uint32_t max_tiles;
+  uint32_t pieces;     // pieces wanted per key/value head
+  uint32_t max_items, max_parts, max_split;
+  uint64_t items, split, acc, ml, bytes;  // offsets from work; bytes in all
+};
+
+// A piece is no shorter than this many units: below it, the joining of partial
+// results costs more than the shorter walk saves.
+constexpr uint32_t kMinUnits = 4;
+
+inline WorkLayout work_layout(const kv_paged_batch& b) {
+  WorkLayout w{};
+  w.group = b.q_heads / b.kv_heads;
+  const uint64_t most = (uint64_t)(b.max_new ? std::min(b.max_new, b.max_tokens) : b.max_tokens) * w.group;
+  const uint32_t busy = std::min(b.n_req, b.max_tokens);
+  // 64 rows of 256 elements from each of four wavefronts would not fit in LDS
+  w.rows = most <= 16 ? 16 : most <= 32 ? 32 : most <= 64 && b.head_dim <= 128 ? 64 : 128;
+  w.max_tiles = w.rows < 128 ? busy : (uint32_t)((uint64_t)b.max_tokens * w.group / 128) + busy;
+  // workgroups that the chip holds at a time, a few times over for the small
+  // tiles, whose pieces are many and short
+  const uint32_t target = w.rows < 128 ? 2048 : 512;
+  w.pieces = (target + b.kv_heads - 1) / b.kv_heads;
+  w.max_items = w.max_tiles + w.pieces;
+  w.max_parts = 2 * w.pieces;
+  w.max_split = w.pieces;
+  auto up = [](uint64_t x) { return (x + 255) / 256 * 256; };
+  w.items = sizeof(WorkHeader);
+  w.split = up(w.items + (uint64_t)w.max_items * sizeof(PieceItem));
+  w.acc = up(w.split + (uint64_t)w.max_split * sizeof(SplitTile));
+  const uint64_t rows = (uint64_t)w.max_parts * b.kv_heads * w.rows;
+  w.ml = up(w.acc + rows * b.head_dim * sizeof(float));
+  w.bytes = up(w.ml + rows * 2 * sizeof(float));
+  return w;
+}
+
+// The frequencies of a rotation, in 2^-64 turns a token.
+struct RopeTable {
+  const uint64_t* turn = nullptr;  // device [rot_dim / 2]
+  float magnitude = 1.0f;
+  uint32_t rot_dim = 0, layout = KV_ROPE_HALF;
+};
+
+kv_status rope_apply(const RopeTable& r, uint32_t dtype, const kv_heads_view& x,
+                     const kv_heads_view& y, const int32_t* pos, uint32_t n_tokens,
+                     uint32_t n_heads, uint32_t head_dim, bool backward, hipStream_t s);
+kv_status paged_plan(const kv_paged_batch& b, const WorkLayout& w, hipStream_t s);
+// r NULL: no rotation
+kv_status paged_append(const kv_paged_batch& b, const kv_paged_cache& c, const RopeTable* r,
+                       uint32_t dtype, const kv_heads_view& q, const kv_heads_view& q_out,
+                       const kv_heads_view& k, const kv_heads_view& v, hipStream_t s);
+kv_status paged_attention(const kv_paged_batch& b, const WorkLayout& w, const kv_paged_cache& c,
+                          uint32_t dtype, const kv_heads_view& q, const kv_heads_view& out,
+                          float* lse, float scale, hipStream_t s);
+
+}  // namespace kv

@@ -1,0 +1,256 @@
+"""ctypes binding of the paged-cache operators (include/kvpaged.h).
+
+As in :mod:`.kvcfg`, every computation runs in the HIP library: this module
+checks tensors, holds the arrays of a step's batch and passes pointers.  One
+serving step is
+
+    plan = Plan(n_req, max_tokens, block_size, max_blocks, q_heads, kv_heads, head_dim, max_new=...)
+    kv_paged_plan(plan, ctx_len, new_len, table, free_list)          # once a step
+    kv_paged_append(plan, cache, k, v, q=q, q_out=q, rope=rope)      # every layer
+    kv_paged_attention(plan, cache, q, out=out)
+"""
+from __future__ import annotations
+
+import ctypes
+
+from .kvcfg import KV_ERR_INVALID, KV_ERR_UNSUPPORTED, KV_OK, LIB, KvError, _check, _stream  # noqa: F401
+
+KV_DT_BF16, KV_DT_F16, KV_DT_FP8 = 0, 1, 2
+KV_ROPE_HALF, KV_ROPE_INTERLEAVED = 0, 1
+KV_ROPE_PLAIN, KV_ROPE_LINEAR, KV_ROPE_BY_PARTS = 0, 1, 2
+KV_PLAN_BAD_LENGTH, KV_PLAN_TOKENS, KV_PLAN_BLOCKS = 1, 2, 4
+KV_PAGED_MAX_REQ, KV_PAGED_MAX_TOKENS = 4096, 524288
+
+_u64, _u32, _i64, _f64, _vp = (ctypes.c_uint64, ctypes.c_uint32, ctypes.c_int64, ctypes.c_double,
+                               ctypes.c_void_p)
+
+
+class kv_rope_desc(ctypes.Structure):
+    _fields_ = [("rot_dim", _u32), ("layout", _u32), ("scaling", _u32), ("original_len", _u32),
+                ("base", _f64), ("factor", _f64), ("fast", _f64), ("slow", _f64),
+                ("magnitude", _f64)]
+
+
+class kv_heads_view(ctypes.Structure):
+    _fields_ = [("ptr", _vp), ("token_stride", _i64), ("head_stride", _i64)]
+
+
+class kv_paged_batch(ctypes.Structure):
+    _fields_ = [("n_req", _u32), ("max_tokens", _u32), ("max_new", _u32), ("block_size", _u32),
+                ("max_blocks", _u32), ("q_heads", _u32), ("kv_heads", _u32), ("head_dim", _u32),
+                ("window", _u32), ("n_free", _u32), ("ctx_len", _vp), ("new_len", _vp),
+                ("table", _vp), ("free_list", _vp), ("q_start", _vp), ("kv_len", _vp),
+                ("slot", _vp), ("pos", _vp), ("result", _vp), ("work", _vp), ("work_bytes", _u64)]
+
+
+class kv_paged_cache(ctypes.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("k_block_stride", _i64), ("v_block_stride", _i64),
+                ("n_blocks", _u32), ("dtype", _u32), ("k_scale", _vp), ("v_scale", _vp)]
+
+
+EXPORTS = ("kv_rope_create", "kv_rope_free", "kv_rope_apply", "kv_paged_work_bytes",
+           "kv_paged_plan", "kv_paged_append", "kv_paged_attention")
+
+_P = ctypes.POINTER
+LIB.kv_rope_create.argtypes = [_P(kv_rope_desc), _P(_vp)]
+LIB.kv_rope_free.argtypes = [_vp]
+LIB.kv_rope_apply.argtypes = [_vp, _u32, kv_heads_view, kv_heads_view, _vp, _u32, _u32, _u32,
+                              ctypes.c_int, _vp]
+LIB.kv_paged_work_bytes.argtypes = [_P(kv_paged_batch), _P(_u64)]
+LIB.kv_paged_plan.argtypes = [_P(kv_paged_batch), _vp]
+LIB.kv_paged_append.argtypes = [_P(kv_paged_batch), _P(kv_paged_cache), _vp, _u32, kv_heads_view,
+                                kv_heads_view, kv_heads_view, kv_heads_view, _vp]
+LIB.kv_paged_attention.argtypes = [_P(kv_paged_batch), _P(kv_paged_cache), _u32, kv_heads_view,
+                                   kv_heads_view, _vp, ctypes.c_float, _vp]
+for _name in EXPORTS:
+    getattr(LIB, _name).restype = ctypes.c_int
+
+
+def _types():
+    import torch
+    return {torch.bfloat16: KV_DT_BF16, torch.float16: KV_DT_F16, torch.float8_e4m3fn: KV_DT_FP8}
+
+
+_TYPES = _types()
+_NO_VIEW = kv_heads_view()
+
+
+def _dtype(t, name):
+    d = _TYPES.get(t.dtype)
+    if d is None or d == KV_DT_FP8:
+        raise ValueError(f"{name} has dtype {t.dtype}; expected bfloat16 or float16")
+    return d
+
+
+def _view(t, name, tokens, heads, dim, dtype=None):
+    """[tokens, heads, dim] with contiguous elements, at least `tokens` rows."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    s = t.shape
+    if len(s) != 3 or s[0] < tokens or s[1] != heads or s[2] != dim:
+        raise ValueError(f"{name} has shape {tuple(s)}; the call needs [>={tokens}, {heads}, {dim}]")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} has dtype {t.dtype}; expected {dtype}")
+    st = t.stride()
+    if st[2] != 1:
+        raise ValueError(f"{name}: a head's elements must be contiguous")
+    return kv_heads_view(t.data_ptr(), st[0], st[1])
+
+
+def _array(t, name, dtype, numel):
+    """A contiguous CUDA tensor of this dtype with at least `numel` elements."""
+    if not t.is_cuda or t.dtype != dtype or not t.is_contiguous() or t.numel() < numel:
+        raise ValueError(f"{name} must be a contiguous CUDA {dtype} tensor of at least {numel} elements")
+    return t.data_ptr()
+
+
+class Rope:
+    """Rotary positions over the first `rot_dim` elements of a head (owns the
+    kv_rope handle, on the current device)."""
+
+    def __init__(self, rot_dim, base=10000.0, layout=KV_ROPE_HALF, scaling=KV_ROPE_PLAIN,
+                 factor=1.0, original_len=0, fast=32.0, slow=1.0, magnitude=1.0):
+        self.handle = None
+        d = kv_rope_desc(rot_dim, layout, scaling, original_len, base, factor, fast, slow, magnitude)
+        h = _vp()
+        _check(LIB.kv_rope_create(ctypes.byref(d), ctypes.byref(h)))
+        self.handle = h
+
+    def free(self):
+        if self.handle is not None:
+            h, self.handle = self.handle, None
+            _check(LIB.kv_rope_free(h))
+
+    def __del__(self):
+        try:
+            if self.handle is not None:
+                LIB.kv_rope_free(self.handle)
+        except Exception:
+            pass
+
+
+def kv_rope_apply(rope: Rope, x, pos, out=None, backward=False, stream=None):
+    """x: [tokens, heads, dim] bfloat16 / float16 at any token and head stride;
+    pos: int32 [tokens]; out: like x (may be x), made when None.  Returns out."""
+    import torch
+    n, heads, dim = x.shape
+    if out is None:
+        out = torch.empty((n, heads, dim), dtype=x.dtype, device=x.device)
+    vx, vy = _view(x, "x", n, heads, dim), _view(out, "out", n, heads, dim, x.dtype)
+    _check(LIB.kv_rope_apply(rope.handle, _dtype(x, "x"), vx, vy,
+                             _array(pos, "pos", torch.int32, n), n, heads, dim,
+                             1 if backward else 0, _stream(stream)))
+    return out
+
+
+class Plan:
+    """The arrays of one step's batch.  Sizes are fixed, so a plan can be filled
+    again for every step, also inside a captured graph; the device arrays
+    q_start, kv_len, slot, pos and result are valid once the stream has
+    completed kv_paged_plan.  It serves one stream at a time."""
+
+    def __init__(self, n_req, max_tokens, block_size, max_blocks, q_heads, kv_heads, head_dim,
+                 max_new=None, window=0, device="cuda"):
+        import torch
+        b = self.batch = kv_paged_batch()
+        b.n_req, b.max_tokens, b.max_new = int(n_req), int(max_tokens), int(max_new or 0)
+        b.block_size, b.max_blocks = int(block_size), int(max_blocks)
+        b.q_heads, b.kv_heads, b.head_dim, b.window = int(q_heads), int(kv_heads), int(head_dim), int(window)
+        size = _u64()
+        _check(LIB.kv_paged_work_bytes(ctypes.byref(b), ctypes.byref(size)))
+        self.q_start = torch.empty(b.n_req + 1, dtype=torch.int32, device=device)
+        self.kv_len = torch.empty(b.n_req, dtype=torch.int32, device=device)
+        self.slot = torch.empty(b.max_tokens, dtype=torch.int64, device=device)
+        self.pos = torch.empty(b.max_tokens, dtype=torch.int32, device=device)
+        self.result = torch.empty(4, dtype=torch.int32, device=device)
+        self.work = torch.empty(size.value, dtype=torch.uint8, device=device)
+        b.q_start, b.kv_len = self.q_start.data_ptr(), self.kv_len.data_ptr()
+        b.slot, b.pos, b.result = self.slot.data_ptr(), self.pos.data_ptr(), self.result.data_ptr()
+        b.work, b.work_bytes = self.work.data_ptr(), size.value
+        self.ref = ctypes.byref(b)
+        self.inputs = None  # kept alive: the later calls of the step read the table
+
+
+def kv_paged_plan(plan: Plan, ctx_len, new_len, table, free_list=None, stream=None):
+    """ctx_len, new_len: int32 [n_req]; table: int32 [n_req, max_blocks], written
+    where a request takes new blocks from free_list (int32), read otherwise."""
+    import torch
+    b = plan.batch
+    if table.dim() != 2 or table.shape[1] != b.max_blocks:
+        raise ValueError(f"table has shape {tuple(table.shape)}; the plan's rows have {b.max_blocks} blocks")
+    i32 = torch.int32
+    b.ctx_len = _array(ctx_len, "ctx_len", i32, b.n_req)
+    b.new_len = _array(new_len, "new_len", i32, b.n_req)
+    b.table = _array(table, "table", i32, b.n_req * b.max_blocks)
+    b.n_free = 0 if free_list is None else free_list.numel()
+    # an empty tensor has no address, and NULL would mean that table names every block
+    b.free_list = None if free_list is None else _array(free_list, "free_list", i32, 0) or b.result
+    plan.inputs = (ctx_len, new_len, table, free_list)
+    _check(LIB.kv_paged_plan(plan.ref, _stream(stream)))
+
+
+class Cache:
+    """A layer's cache: k [n_blocks, kv_heads, block_size, head_dim], v [n_blocks,
+    kv_heads, head_dim, block_size]; blocks may lie at any stride, each block is
+    contiguous.  float8_e4m3fn caches take k_scale, v_scale: float32 [kv_heads]."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        import torch
+        if k.dim() != 4 or v.dim() != 4 or not k.is_cuda or not v.is_cuda:
+            raise ValueError("k and v must be CUDA tensors of four dimensions")
+        n, heads, block, dim = k.shape
+        if tuple(v.shape) != (n, heads, dim, block) or v.dtype != k.dtype or k.dtype not in _TYPES:
+            raise ValueError(f"v has shape {tuple(v.shape)} and dtype {v.dtype}, k {tuple(k.shape)} and {k.dtype}")
+        if k.stride()[1:] != (block * dim, dim, 1) or v.stride()[1:] != (dim * block, block, 1):
+            raise ValueError("a block of the cache must be contiguous")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.shape = (heads, block, dim)
+        one = heads * block * dim  # the stride of a cache of one block says nothing
+        c = self.c = kv_paged_cache()
+        c.k, c.v = k.data_ptr(), v.data_ptr()
+        c.k_block_stride = k.stride(0) if n > 1 else one
+        c.v_block_stride = v.stride(0) if n > 1 else one
+        c.n_blocks, c.dtype = n, _TYPES[k.dtype]
+        c.k_scale = None if k_scale is None else _array(k_scale, "k_scale", torch.float32, heads)
+        c.v_scale = None if v_scale is None else _array(v_scale, "v_scale", torch.float32, heads)
+        self.ref = ctypes.byref(c)
+
+
+def _fits(plan, cache):
+    b = plan.batch
+    if cache.shape != (b.kv_heads, b.block_size, b.head_dim):
+        raise ValueError(f"the cache's heads, block and head size are {cache.shape}; "
+                         f"the plan's {(b.kv_heads, b.block_size, b.head_dim)}")
+    if plan.inputs is None:
+        raise ValueError("the plan is empty: call kv_paged_plan first")
+    return b
+
+
+def kv_paged_append(plan: Plan, cache: Cache, k, v, q=None, q_out=None, rope: Rope | None = None,
+                    stream=None):
+    """k, v: [>=max_tokens, kv_heads, dim]; q, q_out: [>=max_tokens, q_heads, dim]
+    (q_out may be q) or None."""
+    b = _fits(plan, cache)
+    n, dim = b.max_tokens, b.head_dim
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
+    vk, vv = _view(k, "k", n, b.kv_heads, dim), _view(v, "v", n, b.kv_heads, dim, k.dtype)
+    vq = _NO_VIEW if q is None else _view(q, "q", n, b.q_heads, dim, k.dtype)
+    vo = _NO_VIEW if q is None else _view(q_out, "q_out", n, b.q_heads, dim, k.dtype)
+    _check(LIB.kv_paged_append(plan.ref, cache.ref, None if rope is None else rope.handle,
+                               _dtype(k, "k"), vq, vo, vk, vv, _stream(stream)))
+
+
+def kv_paged_attention(plan: Plan, cache: Cache, q, out=None, lse=None, scale=None, stream=None):
+    """q, out: [>=max_tokens, q_heads, dim]; lse: float32 [>=max_tokens, q_heads] or
+    None; scale: dim ** -0.5 when None.  Returns out."""
+    import torch
+    b = _fits(plan, cache)
+    n, heads, dim = b.max_tokens, b.q_heads, b.head_dim
+    if out is None:
+        out = torch.empty((n, heads, dim), dtype=q.dtype, device=q.device)
+    vq, vo = _view(q, "q", n, heads, dim), _view(out, "out", n, heads, dim, q.dtype)
+    pl = None if lse is None else _array(lse, "lse", torch.float32, n * heads)
+    _check(LIB.kv_paged_attention(plan.ref, cache.ref, _dtype(q, "q"), vq, vo, pl,
+                                  dim ** -0.5 if scale is None else scale, _stream(stream)))
+    return out

@@ -1,0 +1,176 @@
+"""The paged-cache library's boundary without a device: header and binding agree,
+and bad arguments are refused before any device work."""
+import ctypes
+import os
+import re
+import subprocess
+import tempfile
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HEADER = os.path.join(ROOT, "include", "kvpaged.h")
+
+
+def batch(K, **more):
+    """Plausible sizes and pointers (never dereferenced: every call here is refused)."""
+    b = K.kv_paged_batch(n_req=4, max_tokens=4, max_new=1, block_size=16, max_blocks=8, q_heads=8, kv_heads=2,
+                         head_dim=64, window=0)
+    size = ctypes.c_uint64()
+    assert K.LIB.kv_paged_work_bytes(ctypes.byref(b), ctypes.byref(size)) == K.KV_OK
+    for f in ("ctx_len", "new_len", "table", "q_start", "kv_len", "slot", "pos", "result", "work"):
+        setattr(b, f, 0x1000)
+    b.work_bytes = size.value
+    for k, v in more.items():
+        setattr(b, k, v)
+    return b
+
+
+def cache(K, **more):
+    c = K.kv_paged_cache(k=0x1000, v=0x1000, k_block_stride=2 * 16 * 64, v_block_stride=2 * 16 * 64, n_blocks=4,
+                         dtype=K.KV_DT_BF16)
+    for k, v in more.items():
+        setattr(c, k, v)
+    return c
+
+
+def view(K, ptr=0x1000, token=512, head=64):
+    return K.kv_heads_view(ptr, token, head)
+
+
+def refused(K, status, *words):
+    assert status == K.KV_ERR_INVALID, status
+    msg = K.LIB.kv_last_error().decode()
+    assert all(w in msg for w in words), msg
+
+
+def test_header_and_binding_name_the_same_functions():
+    from paper_2603_08739_amd import kvpaged as K
+    text = open(HEADER).read()
+    names = sorted(set(re.findall(r"^kv_status (kv_\w+)\s*\(", text, re.M)))
+    assert names == sorted(K.EXPORTS)
+    for n in names:
+        assert hasattr(K.LIB, n)
+
+
+def test_struct_layouts_match_header():
+    from paper_2603_08739_amd import kvpaged as K
+    structs = {"kv_rope_desc": ["rot_dim", "base", "magnitude"], "kv_heads_view": ["ptr", "token_stride", "head_stride"],
+               "kv_paged_batch": ["n_req", "window", "n_free", "ctx_len", "free_list", "slot", "work", "work_bytes"],
+               "kv_paged_cache": ["k", "k_block_stride", "n_blocks", "dtype", "v_scale"]}
+    lines, want = [], []
+    for s, fields in structs.items():
+        lines.append(f'printf("%zu\\n", sizeof({s}));')
+        want.append(ctypes.sizeof(getattr(K, s)))
+        for f in fields:
+            lines.append(f'printf("%zu\\n", offsetof({s}, {f}));')
+            want.append(getattr(getattr(K, s), f).offset)
+    src = '#include <stddef.h>\n#include <stdio.h>\n#include "kvpaged.h"\nint main(void) {' + "\n".join(lines) + "return 0;}"
+    with tempfile.TemporaryDirectory() as d:
+        c, exe = os.path.join(d, "t.c"), os.path.join(d, "t")
+        open(c, "w").write(src)
+        subprocess.run(["gcc", "-Wall", "-Werror", "-I", os.path.join(ROOT, "include"), c, "-o", exe], check=True)
+        got = [int(x) for x in subprocess.run([exe], capture_output=True, text=True, check=True).stdout.split()]
+    assert got == want
+
+
+@pytest.mark.parametrize("field, value, word", [
+    ("n_req", 0, "n_req"), ("n_req", 4097, "n_req"), ("max_tokens", 0, "max_tokens"), ("max_tokens", 524289, "max_tokens"),
+    ("block_size", 8, "block_size"), ("block_size", 48, "block_size"), ("block_size", 512, "block_size"), ("max_blocks", 0, "max_blocks"),
+    ("max_blocks", (1 << 26) + 1, "max_blocks"), ("kv_heads", 0, "kv_heads"), ("kv_heads", 3, "q_heads"), ("q_heads", 0, "q_heads"),
+    ("head_dim", 96, "head_dim"), ("window", 1 << 31, "window")])
+def test_sizes_are_refused(field, value, word):
+    from paper_2603_08739_amd import kvpaged as K
+    b, size = batch(K, **{field: value}), ctypes.c_uint64(7)
+    refused(K, K.LIB.kv_paged_work_bytes(ctypes.byref(b), ctypes.byref(size)), word)
+    assert size.value == 7
+    b.work_bytes = 1 << 40
+    refused(K, K.LIB.kv_paged_plan(ctypes.byref(b), None), word)
+
+
+@pytest.mark.parametrize("field", ["ctx_len", "new_len", "table", "q_start", "kv_len", "slot", "pos", "result", "work"])
+def test_pointers_are_refused(field):
+    from paper_2603_08739_amd import kvpaged as K
+    refused(K, K.LIB.kv_paged_plan(ctypes.byref(batch(K, **{field: None})), None), "NULL")
+    refused(K, K.LIB.kv_paged_plan(ctypes.byref(batch(K, **{field: 0x1001})), None), "aligned")
+
+
+def test_work_size_is_checked():
+    from paper_2603_08739_amd import kvpaged as K
+    b = batch(K)
+    b.work_bytes -= 1
+    refused(K, K.LIB.kv_paged_plan(ctypes.byref(b), None), "work_bytes")
+    refused(K, K.LIB.kv_paged_plan(None, None), "NULL")
+
+
+@pytest.mark.parametrize("more, word", [
+    (dict(k=None), "NULL"), (dict(v=0x1008), "16-byte"), (dict(k_block_stride=2 * 16 * 64 - 16), "stride"),
+    (dict(v_block_stride=2 * 16 * 64 + 8), "stride"), (dict(n_blocks=0), "n_blocks"), (dict(dtype=1), "dtype"), (dict(dtype=3), "dtype"),
+    (dict(k_scale=0x1000), "scales")])
+def test_caches_are_refused(more, word):
+    from paper_2603_08739_amd import kvpaged as K
+    b, c, w = batch(K), cache(K, **more), view(K)
+    refused(K, K.LIB.kv_paged_append(ctypes.byref(b), ctypes.byref(c), None, 0, w, w, w, w, None), word)
+    refused(K, K.LIB.kv_paged_attention(ctypes.byref(b), ctypes.byref(c), 0, w, w, None, 1.0, None), word)
+
+
+def test_heads_and_scales_are_refused():
+    from paper_2603_08739_amd import kvpaged as K
+    b, c, w = batch(K), cache(K), view(K)
+    attend = lambda q=w, out=w, lse=None, scale=1.0, dtype=0: K.LIB.kv_paged_attention(  # noqa: E731
+        ctypes.byref(b), ctypes.byref(c), dtype, q, out, lse, scale, None)
+    refused(K, attend(q=view(K, ptr=None)), "NULL")
+    refused(K, attend(out=view(K, ptr=0x1008)), "16-byte")
+    refused(K, attend(q=view(K, token=513)), "strides")
+    refused(K, attend(q=view(K, head=60)), "strides")
+    refused(K, attend(dtype=2), "dtype")
+    refused(K, attend(lse=0x1002), "lse")
+    for s in (0.0, -1.0, float("inf"), float("nan")):
+        refused(K, attend(scale=s), "scale")
+    append = lambda q=w, q_out=w, k=w, v=w, rope=None: K.LIB.kv_paged_append(  # noqa: E731
+        ctypes.byref(b), ctypes.byref(c), rope, 0, q, q_out, k, v, None)
+    refused(K, append(k=view(K, ptr=None)), "NULL")
+    refused(K, append(q_out=view(K, ptr=None)), "NULL")
+    refused(K, append(v=view(K, token=4)), "strides")
+    refused(K, append(rope=0x1000), "rotation")
+
+
+@pytest.mark.parametrize("more, word", [
+    (dict(rot_dim=0), "rot_dim"), (dict(rot_dim=24), "rot_dim"), (dict(rot_dim=272), "rot_dim"), (dict(layout=2), "layout"),
+    (dict(scaling=3), "scaling"), (dict(base=1.0), "base"), (dict(base=float("inf")), "base"), (dict(magnitude=0.0), "magnitude"),
+    (dict(magnitude=float("nan")), "magnitude"), (dict(scaling=1, factor=0.5), "factor"), (dict(scaling=1, factor=float("nan")), "factor"),
+    (dict(scaling=2, factor=4.0, original_len=0), "BY_PARTS"), (dict(scaling=2, factor=4.0, original_len=64, fast=1.0, slow=1.0), "BY_PARTS")])
+def test_rotations_are_refused(more, word):
+    from paper_2603_08739_amd import kvpaged as K
+    with pytest.raises(K.KvError) as e:
+        K.Rope(**{"rot_dim": 64, **more})
+    assert e.value.status == K.KV_ERR_INVALID and word in str(e.value)
+    h = ctypes.c_void_p(5)
+    assert K.LIB.kv_rope_create(None, ctypes.byref(h)) == K.KV_ERR_INVALID and not h.value
+    assert K.LIB.kv_rope_free(None) == K.KV_OK
+    refused(K, K.LIB.kv_rope_free(0x1000), "live")
+    refused(K, K.LIB.kv_rope_apply(0x1000, 0, view(K), view(K), 0x1000, 1, 1, 64, 0, None), "live")
+
+
+def test_oracle_attention_is_plain_softmax():
+    import torch
+    from oracle import paged as O
+    torch.manual_seed(0)
+    q, k, v = torch.randn(2, 4, 64), torch.randn(3, 2, 16, 64), torch.randn(3, 2, 64, 16)
+    out, lse, _, _ = O.attention(q, k, v, [[2, 0]], [0, 2], [18], 16, 3, 0.125, 0)
+    keys, values = torch.cat([k[2], k[0]], 1).double(), torch.cat([v[2], v[0]], 2).double()
+    for t in range(2):
+        for h in range(4):
+            e = torch.exp(0.125 * (keys[h // 2, :19 + t] @ q[t, h].double()))
+            assert torch.allclose(out[t, h], (e[:, None] * values[h // 2].T[:19 + t]).sum(0) / e.sum(), atol=1e-12)
+            assert abs(lse[t, h] - torch.log(e.sum())) < 1e-12
+
+
+def test_oracle_plan_by_hand():
+    from oracle import paged as O
+    # request 0 goes on inside its block, request 1 is idle, request 2 starts
+    got = O.plan([5, 16, 0], [12, 0, 17], [[3, -1], [4, -1], [-1, -1]], [7, 8, 9], 16, 32, 2, 32)
+    table, start, kv_len, slot, pos, result = got
+    assert table == [[3, 7], [4, -1], [8, 9]] and start == [0, 12, 12, 29] and kv_len == [17, 16, 17]
+    assert slot == [3 * 16 + i for i in range(5, 16)] + [7 * 16] + [8 * 16 + i for i in range(16)] + [9 * 16] + [-1] * 3
+    assert pos == list(range(5, 17)) + list(range(17)) + [0] * 3 and result == [29, 3, 3, 0]
