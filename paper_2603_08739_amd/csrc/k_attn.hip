@@ -24,6 +24,8 @@
 // A weight of 0 times a NaN or an infinity in a masked value would be NaN.  Where
 // a tile holds masked keys, values are therefore looked at: non-finite ones are
 // taken out of the product and added back only to the queries that see them.
+#include <type_traits>
+
 #include "kv_device.h"
 #include "kv_paged.h"
 
@@ -42,7 +44,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 
 struct BF16 {
   static constexpr uint32_t kExp = 0x7f80u;  // exponent bits: all set = not finite
-  static constexpr uint16_t kOne = 0x3f80u;
+  static __device__ __forceinline__ float value(uint16_t u) { return (float)__builtin_bit_cast(__bf16, u); }
   static __device__ __forceinline__ f32x16 mfma32(const uint4& a, const uint4& b, const f32x16& c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
   }
@@ -64,7 +66,7 @@ struct BF16 {
 
 struct F16 {
   static constexpr uint32_t kExp = 0x7c00u;
-  static constexpr uint16_t kOne = 0x3c00u;
+  static __device__ __forceinline__ float value(uint16_t u) { return (float)__builtin_bit_cast(_Float16, u); }
   static __device__ __forceinline__ f32x16 mfma32(const uint4& a, const uint4& b, const f32x16& c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
   }
@@ -114,66 +116,81 @@ __device__ __forceinline__ float other_half(float x) {
   return __builtin_bit_cast(float, lane_id() < 32 ? r[1] : r[0]);
 }
 
-// Masked values that are not finite (see the head of the file).  For one 16-bit
-// operand register: the numbers that are not finite become 0.
+// Masked values that are not finite (see the head of the file).  Bits 15 and 31:
+// whether the halves' exponents are all ones (adding one at the exponent's lowest
+// bit then carries into the sign's place).
 template <class T>
-__device__ __forceinline__ uint32_t not_finite(uint32_t u) {  // all ones in the halves that are not finite
-  uint32_t m = 0;
-  if ((u & T::kExp) == T::kExp) m |= 0xffffu;
-  if (((u >> 16) & T::kExp) == T::kExp) m |= 0xffff0000u;
-  return m;
+__device__ __forceinline__ uint32_t not_finite(uint32_t u) {
+  constexpr uint32_t kExp = T::kExp, kLow = kExp & (~kExp + 1);
+  return ((u & (kExp | kExp << 16)) + (kLow | kLow << 16)) & 0x80008000u;
 }
 template <class T>
-__device__ __forceinline__ bool any_not_finite(const uint4& u) {
-  return (not_finite<T>(u.x) | not_finite<T>(u.y) | not_finite<T>(u.z) | not_finite<T>(u.w)) != 0;
+__device__ __forceinline__ uint32_t not_finite(const uint4& u) {
+  return not_finite<T>(u.x) | not_finite<T>(u.y) | not_finite<T>(u.z) | not_finite<T>(u.w);
+}
+// 0 in the place of what is not finite
+template <class T>
+__device__ __forceinline__ uint32_t finite_part(uint32_t u) {
+  const uint32_t m = not_finite<T>(u);
+  return u & ~(m | (m - (m >> 15)));
 }
 template <class T>
 __device__ __forceinline__ uint4 finite_part(const uint4& u) {
-  return make_uint4(u.x & ~not_finite<T>(u.x), u.y & ~not_finite<T>(u.y), u.z & ~not_finite<T>(u.z),
-                    u.w & ~not_finite<T>(u.w));
+  return make_uint4(finite_part<T>(u.x), finite_part<T>(u.y), finite_part<T>(u.z), finite_part<T>(u.w));
 }
-// 1 where the number is an infinity of this sign or a NaN, else 0
-template <class T>
-__device__ __forceinline__ uint32_t marks(uint32_t u, bool negative) {
-  uint32_t m = 0;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const uint32_t h = (u >> (16 * i)) & 0xffffu;
-    const bool bad = (h & T::kExp) == T::kExp;
-    const bool nan = bad && (h & 0x7fffu) != T::kExp;
-    if (nan || (bad && ((h >> 15) != 0) == negative)) m |= (uint32_t)T::kOne << (16 * i);
-  }
-  return m;
-}
-template <class T>
-__device__ __forceinline__ uint4 marks(const uint4& u, bool negative) {
-  return make_uint4(marks<T>(u.x, negative), marks<T>(u.y, negative), marks<T>(u.z, negative), marks<T>(u.w, negative));
-}
-// what sums of marks under the queries that see the keys add to the output
-__device__ __forceinline__ float marked(float plus, float minus) {
-  const float inf = __builtin_inff();
-  return (plus > 0.0f ? inf : 0.0f) + (minus > 0.0f ? -inf : 0.0f);
+// one value of the cache, unscaled
+template <class T, bool kFp8>
+__device__ __forceinline__ float element(const uint8_t* p) {
+  return T::value(kFp8 ? (uint16_t)T::template widen<false>(*p) : *(const uint16_t*)p);
 }
 
 // ---------------------------------------------------------------------------
 // tiles of 128 rows
 // ---------------------------------------------------------------------------
-// LDS holds 64 keys of K ([64][D]) and V^T ([D][64]) in 16 bits, twice: the next
-// keys are loaded to registers while the present ones are multiplied.  16-byte
-// chunks are stored at chunk ^ row, or at chunk ^ row/2 where two rows of 128 bytes
-// share the 64 banks (V^T, and K of 64 elements), so that the 16-byte reads of a
-// column of rows fall on different banks.
-template <int D>
-__device__ __forceinline__ int k_chunk(int row, int c) {
-  return D == 64 ? row * 8 + (c ^ ((row >> 1) & 7)) : row * (D / 8) + (c ^ (row & 15));
+// 64 keys at a time in LDS, twice: the next ones arrive by loads that go from
+// memory straight to LDS while the present ones are multiplied, with one barrier
+// between.  Wavefront w fetches keys 16w .. 16w + 15, which lie in one block, so the
+// block's number is looked up once for the whole wavefront and a lane's offset
+// never changes.  K is kept by rows of D elements, V^T in four groups of 16 keys
+// by rows of 16 keys; both in the cache's type, 8-bit values are widened after
+// they are read.  16-byte chunks are stored exclusive-ored with bits of their row,
+// so that the reads of a column of rows fall on different banks (the loads place
+// lanes in order, so the lane picks the chunk of memory that belongs there).
+template <int D, int kBytes>
+struct TileLds {
+  static constexpr int kRowChunks = D * kBytes / 16;              // of a row of K
+  static constexpr int kChunks = 64 * kRowChunks;                 // of K, and of V^T
+  static constexpr int kLoads = kChunks / 256;                    // a lane's
+  static constexpr int kShift = kRowChunks >= 16 ? 0 : kRowChunks == 8 ? 1 : 2;  // rows that share the banks: 2^kShift
+  static constexpr int kMask = kRowChunks >= 16 ? 15 : kRowChunks - 1;
+  static __device__ __forceinline__ int k_swap(int row) { return (row >> kShift) & kMask; }
+  static __device__ __forceinline__ int k_at(int row, int chunk) { return row * kRowChunks + (chunk ^ k_swap(row)); }
+  // V^T, element row d of key group g: 16-bit rows are two chunks
+  static __device__ __forceinline__ int v_swap(int d) { return kBytes == 2 ? (d >> 3) & 1 : 0; }
+  static __device__ __forceinline__ int v_at(int g, int d, int chunk) {
+    return kBytes == 2 ? (g * D + d) * 2 + (chunk ^ v_swap(d)) : g * D + d;
+  }
+};
+
+__device__ __forceinline__ void load_to_lds(const uint8_t* from, uint4* to) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                   (__attribute__((address_space(3))) void*)to, 16, 0, 0);
 }
-__device__ __forceinline__ int v_chunk(int row, int c) { return row * 8 + (c ^ ((row >> 1) & 7)); }
+
+// A NaN wins: it stays out of the running maximum and reaches the sum as a weight.
+__device__ __forceinline__ float max2(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ __forceinline__ float max3(float a, float b, float c) { return max2(max2(a, b), c); }
+
+// Rescaling is put off until a maximum rises by more than this (base 2): weights
+// then reach 2^8, which their 16-bit types hold with the same relative rounding.
+constexpr float kSlack = 8.0f;
 
 template <class T, int D, bool kFp8>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attn_tile(AttnArgs a) {
-  constexpr int BK = 64, C = D / 8;
-  constexpr int kKeep = BK * C / 256;  // chunks of K (and of V^T) a thread moves
-  extern __shared__ uint4 lds[];       // [2][K 64*C | V^T D*8]
+  constexpr int BK = 64, kBytes = kFp8 ? 1 : 2;
+  typedef TileLds<D, kBytes> L;
+  __shared__ uint4 k_lds0[L::kChunks], k_lds1[L::kChunks], v_lds0[L::kChunks], v_lds1[L::kChunks];
+  __shared__ int mend;
   const uint32_t item = blockIdx.x / a.kv_heads, head = blockIdx.x % a.kv_heads;
   if ((int)item >= a.head->n_items) return;
   const PieceItem it = a.items[item];
@@ -187,11 +204,15 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attn_tile(AttnArgs a)
   const int token = safe_row / (int)G, gh = safe_row - token * (int)G;
   const int qpos = it.ctx + token;
   const bool wave_on = it.row0 + 32 * wave < it.row_end;
+  // Operand step s of the first product: elements 16*s + 8*half + 0..7 of a 16-bit
+  // cache; of an 8-bit one, whose 16-byte chunk serves two steps, 32*(s/2) + 16*half
+  // + 8*(s%2) + 0..7
   uint4 qf[D / 16];
   {
-    const uint16_t* p = a.q + (int64_t)(it.q_start + token) * a.qt + (int64_t)(head * G + gh) * a.qh + 8 * half;
+    const uint16_t* p = a.q + (int64_t)(it.q_start + token) * a.qt + (int64_t)(head * G + gh) * a.qh;
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s) qf[s] = *(const uint4*)(p + 16 * s);
+    for (int s = 0; s < D / 16; ++s)
+      qf[s] = *(const uint4*)(p + (kFp8 ? 32 * (s / 2) + 16 * half + 8 * (s % 2) : 16 * s + 8 * half));
   }
   // positions of the wave's first and last queries
   const int first_pos = it.ctx + (it.row0 + 32 * wave) / (int)G;
@@ -207,182 +228,186 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attn_tile(AttnArgs a)
 
   const int32_t* table = a.table + (uint64_t)it.req * a.max_blocks;
   const int bs_mask = (1 << a.shift) - 1;
-  constexpr int kBytes = kFp8 ? 1 : 2;
-  const int64_t k_head = (int64_t)head * D * kBytes << a.shift;
-  uint4 kr[kKeep], vr[kKeep];
-  uint64_t next_valid = 0;
-
-  // loads 64 keys from `key` on to registers; keys without a block read block 0
-  auto fetch = [&](int key) {
-    {
-      const int kk = key + lane;
-      int page = -1;
-      if (kk < it.key_end) page = table[kk >> a.shift];
-      next_valid = __ballot(page >= 0 && page < (int)a.n_blocks);
-    }
+  const uint8_t* k_base = a.k + ((int64_t)head * D * kBytes << a.shift);
+  const uint8_t* v_base = a.v + ((int64_t)head * D * kBytes << a.shift);
+  // this lane's places in a group of 16 keys
+  uint32_t k_from[L::kLoads], v_from[L::kLoads];
 #pragma unroll
-    for (int i = 0; i < kKeep; ++i) {
-      const int chunk = tid + 256 * i;
-      const int r = chunk / C, cc = chunk % C;
-      const int kk = min(key + r, it.key_end - 1);
-      int page = table[kk >> a.shift];
-      if (page < 0 || page >= (int)a.n_blocks) page = 0;
-      const uint8_t* p = a.k + page * a.k_block * kBytes + k_head + ((int64_t)(kk & bs_mask) * D + cc * 8) * kBytes;
+  for (int i = 0; i < L::kLoads; ++i) {
+    const int x = 64 * i + lane;  // chunk of the group
+    const int r = x / L::kRowChunks;
+    k_from[i] = (uint32_t)(r * L::kRowChunks + ((x % L::kRowChunks) ^ L::k_swap(16 * wave + r))) * 16;
+    const int d = kBytes == 2 ? x / 2 : x;
+    v_from[i] = (uint32_t)((d * kBytes) << a.shift) + (kBytes == 2 ? (uint32_t)((x & 1) ^ L::v_swap(d)) * 16 : 0u);
+  }
+  // A tile's four groups have one block each: lane i looks up that of group i % 4,
+  // two tiles ahead.  Groups past the last key read its group again, missing blocks
+  // block 0.
+  auto there = [&](int page) { return page >= 0 && page < (int)a.n_blocks; };
+  auto look_up = [&](int key) { return table[min(key + 16 * (lane & 3), it.key_end - 1) >> a.shift]; };
+  auto fetch = [&](int key, int pages, uint4* lk, uint4* lv) {
+    const int k16 = min(key + 16 * wave, (it.key_end - 1) & ~15);
+    int page = __builtin_amdgcn_readlane(pages, wave);
+    if (!there(page)) page = 0;
+    const uint8_t* kp = k_base + page * a.k_block * kBytes + (int64_t)(k16 & bs_mask) * D * kBytes;
+    const uint8_t* vp = v_base + page * a.v_block * kBytes + (k16 & bs_mask) * kBytes;
+#pragma unroll
+    for (int i = 0; i < L::kLoads; ++i) load_to_lds(kp + k_from[i], lk + (wave * L::kLoads + i) * 64);
+#pragma unroll
+    for (int i = 0; i < L::kLoads; ++i) load_to_lds(vp + v_from[i], lv + (wave * L::kLoads + i) * 64);
+  };
+
+  // The lane's results e = 0..15 of the first product's block n are keys 32*n + 16*(e/8)
+  // + 8*half + e%8 (8 bits: 32*n + 16*half + e); the row of K that gives them:
+  const int krow = kFp8 ? ((col & 4) << 2) | ((col & 24) >> 1) | (col & 3) : (col & 19) | ((col & 4) << 1) | ((col & 8) >> 1);
+  auto v_frag = [&](const uint4* lv, int i, int kb) {
+    if (kFp8) {
+      const uint4 u = lv[L::v_at((kb & ~1) + half, 32 * i + col, 0)];
+      return kb & 1 ? widen8<T>(u.z, u.w) : widen8<T>(u.x, u.y);
+    }
+    return lv[L::v_at(kb, 32 * i + col, half)];
+  };
+
+  // Values that are not finite leave V^T before anyone multiplies by it, where some
+  // query masks a key of the group; `mend` says that one belonged to a key that
+  // some query sees (a block's unused end, say, may hold anything).
+  const int tile_first = it.ctx + it.row0 / (int)G, tile_last = it.ctx + (min(it.row0 + 128, it.row_end) - 1) / (int)G;
+  auto clean = [&](int key, uint32_t groups, uint4* lv) {
+    const int k16 = key + 16 * wave;
+    const bool here = (groups >> wave) & 1;
+    if (here && k16 + 15 <= tile_first && k16 > tile_last - window && k16 + 15 < it.key_end) return;
+    uint32_t any = 0;
+#pragma unroll
+    for (int i = 0; i < L::kLoads; ++i) {
+      const uint4 u = lv[(wave * L::kLoads + i) * 64 + lane];
+      any |= kFp8 ? not_finite<T>(widen8<T>(u.x, u.y)) | not_finite<T>(widen8<T>(u.z, u.w)) : not_finite<T>(u);
+    }
+    if (!__any(any != 0)) return;
+    bool seen = false;
+#pragma unroll 1
+    for (int i = 0; i < L::kLoads * 16 / kBytes; ++i) {
+      const int chunk = (wave * L::kLoads + i / (16 / kBytes)) * 64 + lane, j = i % (16 / kBytes);
+      uint8_t* e = (uint8_t*)(lv + chunk) + j * kBytes;
+      if (__builtin_isfinite(element<T, kFp8>(e))) continue;
+      if (kFp8)
+        *e = 0;
+      else
+        *(uint16_t*)e = 0;
+      // chunk 2*d + (half of the group ^ swap), or one chunk for the whole group
+      const int x = chunk - wave * L::kLoads * 64;
+      const int at = k16 + (kBytes == 2 ? 8 * ((x & 1) ^ L::v_swap(x >> 1)) : 0) + j;
+      seen |= here && at <= tile_last && at > tile_first - window && at < it.key_end;
+    }
+    if (__any(seen)) mend = 1;
+  };
+
+  int pages = look_up(it.key_begin), next_pages = look_up(it.key_begin + BK);
+  auto step = [&](int key, const uint4* lk, uint4* lv, uint4* next_k, uint4* next_v) __attribute__((always_inline)) {
+    // groups of 16 keys that are there
+    const uint32_t valid = (uint32_t)__ballot(there(pages) && key + 16 * (lane & 3) < it.key_end) & 15u;
+    // This wavefront's loads to LDS have arrived.  They are counted with the loads
+    // from memory, which the barrier itself does not wait for.
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    clean(key, valid, lv);
+    __syncthreads();  // everybody's have, and nobody reads the other keys any more
+    if (key + BK < it.key_end) fetch(key + BK, next_pages, next_k, next_v);
+    pages = next_pages;
+    next_pages = look_up(key + 2 * BK);
+    if (!wave_on || key > last_pos || key + BK <= first_pos - window + 1) return;
+    const bool edge = key + BK - 1 > first_pos || key <= last_pos - window || valid != 15;
+    f32x16 s[2];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      s[n] = f32x16{};
       if (kFp8) {
-        const uint2 u = *(const uint2*)p;
-        kr[i].x = u.x, kr[i].y = u.y;
-      } else {
-        kr[i] = *(const uint4*)p;
-      }
-    }
-    {
-      const int kk = key + 8 * (tid & 7);
-      // a run of 8 keys that begins past the last one reads the last one's run
-      const int k8 = min(kk, (it.key_end - 1) & ~7);
-      int page = table[k8 >> a.shift];
-      if (page < 0 || page >= (int)a.n_blocks) page = 0;
-      const uint8_t* p = a.v + page * a.v_block * kBytes + k_head + (k8 & bs_mask) * kBytes;
 #pragma unroll
-      for (int i = 0; i < kKeep; ++i) {
-        const int d = (tid >> 3) + 32 * i;
-        const uint8_t* q = p + ((int64_t)d * kBytes << a.shift);
-        if (kFp8) {
-          const uint2 u = *(const uint2*)q;
-          vr[i].x = u.x, vr[i].y = u.y;
-        } else {
-          vr[i] = *(const uint4*)q;
+        for (int d = 0; d < D / 32; ++d) {
+          const uint4 u = lk[L::k_at(32 * n + krow, 2 * d + half)];
+          s[n] = T::mfma32(widen8<T>(u.x, u.y), qf[2 * d], s[n]);
+          s[n] = T::mfma32(widen8<T>(u.z, u.w), qf[2 * d + 1], s[n]);
         }
+      } else {
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) s[n] = T::mfma32(lk[L::k_at(32 * n + krow, 2 * d + half)], qf[d], s[n]);
       }
     }
-  };
-  auto store = [&](int buf) {
-    uint4* lk = lds + buf * (BK * C + D * 8);
-    uint4* lv = lk + BK * C;
-#pragma unroll
-    for (int i = 0; i < kKeep; ++i) {
-      const int chunk = tid + 256 * i;
-      const uint4 u = kFp8 ? widen8<T>(kr[i].x, kr[i].y) : kr[i];
-      lk[k_chunk<D>(chunk / C, chunk % C)] = u;
-      const uint4 w = kFp8 ? widen8<T>(vr[i].x, vr[i].y) : vr[i];
-      lv[v_chunk((tid >> 3) + 32 * i, tid & 7)] = w;
-    }
-  };
-
-  fetch(it.key_begin);
-  uint64_t valid = next_valid;
-  store(0);
-  __syncthreads();
-  int buf = 0;
-  for (int key = it.key_begin; key < it.key_end; key += BK) {
-    const bool more = key + BK < it.key_end;
-    if (more) fetch(key + BK);
-    if (wave_on && key <= last_pos && key + BK > first_pos - window + 1) {
-      const uint4* lk = lds + buf * (BK * C + D * 8);
-      const uint4* lv = lk + BK * C;
-      // S^T: lane holds keys 32*n + 16*(b/2) + 8*half + 4*(b%2) + i at s[n][4*b + i]
-      f32x16 s[2];
-      const int krow = (col & 19) | ((col & 4) << 1) | ((col & 8) >> 1);
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        s[n] = f32x16{};
-#pragma unroll
-        for (int d = 0; d < D / 16; ++d)
-          s[n] = T::mfma32(lk[k_chunk<D>(32 * n + krow, 2 * d + half)], qf[d], s[n]);
-      }
-      const bool edge = key + BK - 1 > first_pos || key <= last_pos - window || ~valid;
-      uint32_t seen = ~0u;  // bit 16*n + e: this lane's query sees the key of s[n][e]
-      if (edge) {
-        seen = 0;
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int at = 32 * n + 16 * (e >> 3) + 8 * half + (e & 7);
-            const int kk = key + at;
-            const bool ok = kk <= qpos && kk > qpos - window && ((valid >> at) & 1);
-            if (ok)
-              seen |= 1u << (16 * n + e);
-            else
-              s[n][e] = -__builtin_inff();
-          }
-      }
-      float top = -__builtin_inff();
+    if (edge) {
 #pragma unroll
       for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[n][e]);
-      top = fmaxf(top, other_half(top)) * c;
-      const float m_new = fmaxf(m, top);
-      const float sub = m_new == -__builtin_inff() ? 0.0f : m_new;
-      const float alpha = __builtin_amdgcn_exp2f(m - sub);
-      m = m_new;
-      float sum = 0.0f;
-      uint4 p[4];
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-#pragma unroll
         for (int e = 0; e < 16; ++e) {
-          s[n][e] = __builtin_amdgcn_exp2f(fmaf(s[n][e], c, -sub));
-          sum += s[n][e];
+          constexpr int kRun = kFp8 ? 16 : 8;
+          const int at = 32 * n + (kFp8 ? e : 16 * (e >> 3) + (e & 7));  // + kRun * half: the key
+          const int from = key + kRun * half;
+          const bool here = (valid >> (2 * n + (kFp8 ? half : e >> 3))) & 1;
+          s[n][e] = here && at <= qpos - from && at > qpos - window - from ? s[n][e] : -__builtin_inff();
         }
+    }
+    float top = max3(s[0][0], s[0][1], s[1][0]);
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-          p[2 * n + h] = make_uint4(T::pack(s[n][8 * h], s[n][8 * h + 1]), T::pack(s[n][8 * h + 2], s[n][8 * h + 3]),
-                                    T::pack(s[n][8 * h + 4], s[n][8 * h + 5]), T::pack(s[n][8 * h + 6], s[n][8 * h + 7]));
-      }
-      l = l * alpha + sum;
+    for (int e = 2; e < 16; e += 2) top = max3(top, s[0][e], s[0][e + 1]);
+#pragma unroll
+    for (int e = 1; e < 15; e += 2) top = max3(top, s[1][e], s[1][e + 1]);
+    top = max2(top, s[1][15]);
+    top = max2(top, other_half(top)) * c;
+    if (__any(top > m + kSlack)) {
+      const float m_new = fmaxf(m, top);
+      const float alpha = m_new == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
+      m = m_new;
+      l *= alpha;
 #pragma unroll
       for (int i = 0; i < D / 32; ++i)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[i][e] *= alpha;
-      bool bad = false;
-      if (edge) {
-#pragma unroll 1
-        for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-          for (int kb = 0; kb < 4; ++kb) bad |= any_not_finite<T>(lv[v_chunk(32 * i + col, 2 * kb + half)]);
-        bad = __any(bad);
-      }
-      if (!bad) {
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-          for (int kb = 0; kb < 4; ++kb) o[i] = T::mfma32(lv[v_chunk(32 * i + col, 2 * kb + half)], p[kb], o[i]);
-      } else {
-        uint4 sees[4];
-#pragma unroll
-        for (int kb = 0; kb < 4; ++kb) {
-          uint32_t u[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t bits = seen >> (8 * kb + 2 * j);
-            u[j] = (bits & 1 ? (uint32_t)T::kOne : 0u) | (bits & 2 ? (uint32_t)T::kOne << 16 : 0u);
-          }
-          sees[kb] = make_uint4(u[0], u[1], u[2], u[3]);
-        }
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
-          f32x16 plus{}, minus{};
-#pragma unroll
-          for (int kb = 0; kb < 4; ++kb) {
-            const uint4 v = lv[v_chunk(32 * i + col, 2 * kb + half)];
-            o[i] = T::mfma32(finite_part<T>(v), p[kb], o[i]);
-            plus = T::mfma32(marks<T>(v, false), sees[kb], plus);
-            minus = T::mfma32(marks<T>(v, true), sees[kb], minus);
-          }
-#pragma unroll
-          for (int e = 0; e < 16; ++e) o[i][e] += marked(plus[e], minus[e]);
-        }
-      }
     }
-    if (more) {
-      store(buf ^ 1);
-      valid = next_valid;
+    const float sub = m == -__builtin_inff() ? 0.0f : m;
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    uint4 p[4];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        s[n][e] = __builtin_amdgcn_exp2f(fmaf(s[n][e], c, -sub));
+        sum[e & 3] += s[n][e];
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        p[2 * n + h] = make_uint4(T::pack(s[n][8 * h], s[n][8 * h + 1]), T::pack(s[n][8 * h + 2], s[n][8 * h + 3]),
+                                  T::pack(s[n][8 * h + 4], s[n][8 * h + 5]), T::pack(s[n][8 * h + 6], s[n][8 * h + 7]));
     }
-    __syncthreads();
-    buf ^= 1;
-  }
+    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int kb = 0; kb < 4; ++kb) o[i] = T::mfma32(v_frag(lv, i, kb), p[kb], o[i]);
+  };
 
+  if (tid == 0) mend = 0;
+  fetch(it.key_begin, pages, k_lds0, v_lds0);
+  __syncthreads();  // mend
+  for (int key = it.key_begin; key < it.key_end; key += 2 * BK) {
+    step(key, k_lds0, v_lds0, k_lds1, v_lds1);
+    if (key + BK < it.key_end) step(key + BK, k_lds1, v_lds1, k_lds0, v_lds0);
+  }
+  // What was taken out, added to what has been stored for this lane's query (an
+  // infinity or a NaN decides its element whatever the scale).
+  auto add_bad = [&](auto add) {
+#pragma unroll 1
+    for (int key = max(it.key_begin, qpos - window + 1); key < it.key_end && key <= qpos; ++key) {
+      const int page = table[key >> a.shift];
+      if (!there(page)) continue;
+      const uint8_t* vp = v_base + page * a.v_block * kBytes + (key & bs_mask) * kBytes;
+#pragma unroll 1
+      for (int x = 0; x < D / 2; ++x) {
+        const int d = 8 * (x >> 2) + 4 * half + (x & 3);
+        const float v = element<T, kFp8>(vp + ((int64_t)(d * kBytes) << a.shift));
+        if (!__builtin_isfinite(v)) add(d, v);
+      }
+    }
+  };
+
+  __syncthreads();
+  const bool mended = mend != 0;
   l += other_half(l);
   if (row >= it.row_end) return;
   if (it.part >= 0) {
@@ -395,6 +420,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attn_tile(AttnArgs a)
         *(float4*)(acc + 32 * i + 8 * b + 4 * half) =
             make_float4(o[i][4 * b], o[i][4 * b + 1], o[i][4 * b + 2], o[i][4 * b + 3]);
     if (half == 0) *(float2*)(a.ml + at * 2) = make_float2(m, l);
+    if (mended) add_bad([&](int d, float v) { acc[d] += v; });
     return;
   }
   const float v_scale = kFp8 && a.v_scale ? a.v_scale[head] : 1.0f;
@@ -408,6 +434,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attn_tile(AttnArgs a)
                                                              T::pack(o[i][4 * b + 2] * inv, o[i][4 * b + 3] * inv));
   if (a.lse && half == 0)
     a.lse[(int64_t)(it.q_start + token) * a.q_heads + head * G + gh] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+  if (mended) add_bad([&](int d, float v) { op[d] = (uint16_t)T::pack(T::value(op[d]) + v, 0.0f); });
 }
 
 // ---------------------------------------------------------------------------
@@ -420,7 +447,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attn_tile(AttnArgs a)
 // kPer - 1 (kPer = 8 or 16), which is also its run of V^T.  At the end the four
 // wavefronts' results are joined through LDS.
 template <class T, int D, bool kFp8, int NC>
-__global__ __launch_bounds__(256) void k_attn_rows(AttnArgs a) {
+__global__ __launch_bounds__(256, D * NC <= 128 ? 2 : 1) void k_attn_rows(AttnArgs a) {
   constexpr int kPer = kFp8 ? 16 : 8, kKeys = 4 * kPer, kBlocks = kKeys / 16, kSteps = kKeys / 32;
   constexpr int kLoadsK = D / 4 / kPer;  // 16-byte loads of a key row by a lane
   const uint32_t item = blockIdx.x / a.kv_heads, head = blockIdx.x % a.kv_heads;
@@ -430,6 +457,55 @@ __global__ __launch_bounds__(256) void k_attn_rows(AttnArgs a) {
   const int col = lane & 15, g = lane >> 4;
   const uint32_t G = a.group;
   const int rows = it.row_end;  // row0 is 0: one tile a request
+
+  const int32_t* table = a.table + (uint64_t)it.req * a.max_blocks;
+  const int bs_mask = (1 << a.shift) - 1;
+  constexpr int kBytes = kFp8 ? 1 : 2;
+  const int64_t k_head = (int64_t)head * D * kBytes << a.shift;
+  const int last_run = (it.key_end - 1) & ~(kPer - 1);
+  // this lane's keys: rows of K from run kPer * (col / 4), V^T's run kPer * g
+  const int k_run = kPer * (col >> 2), v_run = kPer * g;
+  const int window = a.window ? (int)a.window : 0x40000000;
+  const int first_pos = it.ctx, last_pos = it.ctx + (rows - 1) / (int)G;
+
+  // Blocks are looked up two runs ahead, keys and values loaded one ahead: keys as
+  // soon as the first product has taken the present ones, values after the second.
+  struct Pages {
+    int k, v;
+  };
+  auto there = [&](int page) { return page >= 0 && page < (int)a.n_blocks; };
+  auto look_up = [&](int key) {
+    Pages p;
+    p.k = table[min(key + k_run, last_run) >> a.shift];
+    p.v = table[min(key + v_run, last_run) >> a.shift];
+    return p;
+  };
+  uint4 kf[kBlocks][kLoadsK], vf[D / 16];
+  auto load_k = [&](int key, int page) {
+    const int kk = min(key + k_run, last_run);
+    const uint8_t* kp = a.k + (there(page) ? page : 0) * a.k_block * kBytes + k_head +
+                        ((int64_t)((kk & bs_mask) + (col & 3)) * D + kPer * g) * kBytes;
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+      for (int x = 0; x < kLoadsK; ++x) kf[b][x] = *(const uint4*)(kp + 4 * b * D * kBytes + 4 * kPer * x * kBytes);
+  };
+  auto load_v = [&](int key, int page) {
+    const int kk = min(key + v_run, last_run);
+    const uint8_t* vp = a.v + (there(page) ? page : 0) * a.v_block * kBytes + k_head +
+                        (((int64_t)col << a.shift) + (kk & bs_mask)) * kBytes;
+    const int64_t stride = (int64_t)(16 * kBytes) << a.shift;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) vf[i] = *(const uint4*)(vp + i * stride);
+  };
+  const int first = it.key_begin + kKeys * wave;
+  Pages now{-1, -1}, next{-1, -1};
+  if (first < it.key_end) {
+    now = look_up(first);
+    next = look_up(first + 4 * kKeys);
+    load_k(first, now.k);
+    load_v(first, now.v);
+  }
 
   // Queries: operand step s covers the elements that the lane's key loads hold:
   // load x = elements 4*kPer*x + kPer*g + 0 .. kPer-1
@@ -447,8 +523,6 @@ __global__ __launch_bounds__(256) void k_attn_rows(AttnArgs a) {
       qf[n][s] = *(const uint4*)(p + 4 * kPer * (s / kSub) + 8 * (s % kSub));
     }
   }
-  const int window = a.window ? (int)a.window : 0x40000000;
-  const int first_pos = it.ctx, last_pos = it.ctx + (rows - 1) / (int)G;
   const float k_scale = kFp8 && a.k_scale ? a.k_scale[head] : 1.0f;
   const float c = a.scale * kLog2e * k_scale;
 
@@ -461,140 +535,102 @@ __global__ __launch_bounds__(256) void k_attn_rows(AttnArgs a) {
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) o[n][i] = f32x4{};
   }
+  bool mend = false;
 
-  const int32_t* table = a.table + (uint64_t)it.req * a.max_blocks;
-  const int bs_mask = (1 << a.shift) - 1;
-  constexpr int kBytes = kFp8 ? 1 : 2;
-  const int64_t k_head = (int64_t)head * D * kBytes << a.shift;
-  const int last_run = (it.key_end - 1) & ~(kPer - 1);
-  // this lane's keys: rows of K from run kPer * (col / 4), V^T's run kPer * g
-  const int k_run = kPer * (col >> 2), v_run = kPer * g;
-
-  for (int key = it.key_begin + kKeys * wave; key < it.key_end; key += 4 * kKeys) {
-    const int kk = min(key + k_run, last_run), kv = min(key + v_run, last_run);
-    int k_page = table[kk >> a.shift], v_page = table[kv >> a.shift];
-    const bool k_ok = k_page >= 0 && k_page < (int)a.n_blocks, v_ok = v_page >= 0 && v_page < (int)a.n_blocks;
-    if (!k_ok) k_page = 0;
-    if (!v_ok) v_page = 0;
-    const uint8_t* kp = a.k + k_page * a.k_block * kBytes + k_head + ((int64_t)((kk & bs_mask) + (col & 3)) * D + kPer * g) * kBytes;
-    const uint8_t* vp = a.v + v_page * a.v_block * kBytes + k_head + ((int64_t)(col << a.shift) + (kv & bs_mask)) * kBytes;
-    uint4 kf[kBlocks][kLoadsK], vf[D / 16];
-#pragma unroll
-    for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-      for (int x = 0; x < kLoadsK; ++x) kf[b][x] = *(const uint4*)(kp + 4 * b * D * kBytes + 4 * kPer * x * kBytes);
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) vf[i] = *(const uint4*)(vp + ((int64_t)(16 * i * kBytes) << a.shift));
-
+#pragma unroll 1
+  for (int key = first; key < it.key_end; key += 4 * kKeys) {
+    const bool more = key + 4 * kKeys < it.key_end;
+    const bool v_ok = there(now.v);
     const bool edge = key + kKeys - 1 > first_pos || key <= last_pos - window || __any(!v_ok);
+    // s[n][b][i]: key v_run + 4*b + i of the run, query 16*n + col
+    f32x4 s[NC][kBlocks];
 #pragma unroll
-    for (int n = 0; n < NC; ++n) {
-      // s[b][i]: key v_run + 4*b + i of the run, query 16*n + col
-      f32x4 s[kBlocks];
+    for (int b = 0; b < kBlocks; ++b) {
 #pragma unroll
-      for (int b = 0; b < kBlocks; ++b) {
-        s[b] = f32x4{};
+      for (int n = 0; n < NC; ++n) s[n][b] = f32x4{};
 #pragma unroll
-        for (int x = 0; x < kLoadsK; ++x) {
-          if (kFp8) {
-            s[b] = T::mfma16(widen8<T>(kf[b][x].x, kf[b][x].y), qf[n][2 * x], s[b]);
-            s[b] = T::mfma16(widen8<T>(kf[b][x].z, kf[b][x].w), qf[n][2 * x + 1], s[b]);
-          } else {
-            s[b] = T::mfma16(kf[b][x], qf[n][x], s[b]);
-          }
+      for (int x = 0; x < kLoadsK; ++x) {
+        const uint4 lo = kFp8 ? widen8<T>(kf[b][x].x, kf[b][x].y) : kf[b][x];
+#pragma unroll
+        for (int n = 0; n < NC; ++n) s[n][b] = T::mfma16(lo, qf[n][kFp8 ? 2 * x : x], s[n][b]);
+        if (kFp8) {
+          const uint4 hi = widen8<T>(kf[b][x].z, kf[b][x].w);
+#pragma unroll
+          for (int n = 0; n < NC; ++n) s[n][b] = T::mfma16(hi, qf[n][(2 * x + 1) % (D / 32)], s[n][b]);
         }
       }
-      uint32_t seen = ~0u;  // bit 4*b + i
+    }
+    if (more) load_k(key + 4 * kKeys, next.k);
+    uint4 p[NC][kSteps];
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
       if (edge) {
-        seen = 0;
+        const int from = key + v_run;
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int at = key + v_run + 4 * b + i;
-            const bool ok = v_ok && at <= qpos[n] && at > qpos[n] - window && at < it.key_end;
-            if (ok)
-              seen |= 1u << (4 * b + i);
-            else
-              s[b][i] = -__builtin_inff();
+            const int at = 4 * b + i;
+            const bool ok = v_ok && at <= qpos[n] - from && at > qpos[n] - window - from && at < it.key_end - from;
+            s[n][b][i] = ok ? s[n][b][i] : -__builtin_inff();
           }
       }
-      float top = -__builtin_inff();
+      float top = s[n][0][0];
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) {
+        top = max3(top, s[n][b][0], s[n][b][1]);
+        top = max3(top, s[n][b][2], s[n][b][3]);
+      }
+      top = max2(top, __shfl_xor(top, 16, 64));
+      top = max2(top, other_half(top)) * c;
+      if (__any(top > m[n] + kSlack)) {
+        const float m_new = fmaxf(m[n], top);
+        const float alpha = m_new == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m[n] - m_new);
+        m[n] = m_new;
+        l[n] *= alpha;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[n][i][e] *= alpha;
+      }
+      const float sub = m[n] == -__builtin_inff() ? 0.0f : m[n];
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) top = fmaxf(top, s[b][i]);
-      top = fmaxf(top, __shfl_xor(top, 16, 64));
-      top = fmaxf(top, other_half(top)) * c;
-      const float m_new = fmaxf(m[n], top);
-      const float sub = m_new == -__builtin_inff() ? 0.0f : m_new;
-      const float alpha = __builtin_amdgcn_exp2f(m[n] - sub);
-      m[n] = m_new;
-      float sum = 0.0f;
+        for (int i = 0; i < 4; ++i) s[n][b][i] = __builtin_amdgcn_exp2f(fmaf(s[n][b][i], c, -sub));
 #pragma unroll
-      for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c, -sub));
-          sum += s[b][i];
-        }
-      uint4 p[kSteps];
+      for (int b = 0; b < kBlocks; ++b) l[n] += (s[n][b][0] + s[n][b][1]) + (s[n][b][2] + s[n][b][3]);
 #pragma unroll
       for (int e = 0; e < kSteps; ++e)
-        p[e] = make_uint4(T::pack(s[2 * e][0], s[2 * e][1]), T::pack(s[2 * e][2], s[2 * e][3]),
-                          T::pack(s[2 * e + 1][0], s[2 * e + 1][1]), T::pack(s[2 * e + 1][2], s[2 * e + 1][3]));
-      l[n] = l[n] * alpha + sum;
-      bool bad = false;
-      if (edge) {
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) {
-          if (kFp8) {
-            bad |= any_not_finite<T>(widen8<T>(vf[i].x, vf[i].y)) || any_not_finite<T>(widen8<T>(vf[i].z, vf[i].w));
-          } else {
-            bad |= any_not_finite<T>(vf[i]);
-          }
-        }
-        bad = __any(bad);
-      }
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i) {
-        uint4 v[kSteps];
-        if (kFp8) {
-          v[0] = widen8<T>(vf[i].x, vf[i].y);
-          v[kSteps - 1] = widen8<T>(vf[i].z, vf[i].w);
-        } else {
-          v[0] = vf[i];
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[n][i][e] *= alpha;
-        if (!bad) {
-#pragma unroll
-          for (int e = 0; e < kSteps; ++e) o[n][i] = T::mfma16(v[e], p[e], o[n][i]);
-        } else {
-          f32x4 plus{}, minus{};
-#pragma unroll
-          for (int e = 0; e < kSteps; ++e) {
-            uint32_t u[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const uint32_t bits = seen >> (8 * e + 2 * j);
-              u[j] = (bits & 1 ? (uint32_t)T::kOne : 0u) | (bits & 2 ? (uint32_t)T::kOne << 16 : 0u);
-            }
-            const uint4 sees = make_uint4(u[0], u[1], u[2], u[3]);
-            o[n][i] = T::mfma16(finite_part<T>(v[e]), p[e], o[n][i]);
-            plus = T::mfma16(marks<T>(v[e], false), sees, plus);
-            minus = T::mfma16(marks<T>(v[e], true), sees, minus);
-          }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[n][i][e] += marked(plus[e], minus[e]);
-        }
-      }
+        p[n][e] = make_uint4(T::pack(s[n][2 * e][0], s[n][2 * e][1]), T::pack(s[n][2 * e][2], s[n][2 * e][3]),
+                             T::pack(s[n][2 * e + 1][0], s[n][2 * e + 1][1]), T::pack(s[n][2 * e + 1][2], s[n][2 * e + 1][3]));
     }
+    uint32_t any = 0;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+      for (int e = 0; e < kSteps; ++e) {
+        uint4 v = kFp8 ? e ? widen8<T>(vf[i].z, vf[i].w) : widen8<T>(vf[i].x, vf[i].y) : vf[i];
+        if (edge) {
+          any |= not_finite<T>(v);
+          v = finite_part<T>(v);
+        }
+#pragma unroll
+        for (int n = 0; n < NC; ++n) o[n][i] = T::mfma16(v, p[n][e], o[n][i]);
+        if (NC > 1 && e == kSteps - 1) __builtin_amdgcn_sched_barrier(0);
+      }
+    // Of a key that some query sees?  (A block's unused end may hold anything; a
+    // run that only begins among the seen is looked at again below.)
+    if (edge) mend = mend || __any(any != 0 && v_ok && key + v_run <= last_pos && key + v_run + kPer > first_pos - window + 1);
+    if (more) load_v(key + 4 * kKeys, next.v);
+    now = next;
+    if (key + 8 * kKeys < it.key_end) next = look_up(key + 8 * kKeys);
   }
 
   // join the wavefronts
   constexpr int kPad = D + 4;
   extern __shared__ float flds[];  // [4][16 * NC][kPad], then [4][16 * NC][2]
+  __shared__ int mends[4];
   float* stat = flds + 4 * 16 * NC * kPad;
 #pragma unroll
   for (int n = 0; n < NC; ++n) {
@@ -608,7 +644,9 @@ __global__ __launch_bounds__(256) void k_attn_rows(AttnArgs a) {
       stat[2 * at + 1] = l[n];
     }
   }
+  if (lane == 0) mends[wave] = mend;
   __syncthreads();
+  mend = mends[0] | mends[1] | mends[2] | mends[3];
   const float v_scale = kFp8 && a.v_scale ? a.v_scale[head] : 1.0f;
   constexpr int kQuads = D / 4;
   for (int x = tid; x < rows * kQuads; x += 256) {
@@ -628,13 +666,27 @@ __global__ __launch_bounds__(256) void k_attn_rows(AttnArgs a) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum[e] = fmaf(f, v[e], sum[e]);
     }
+    const int token = r / (int)G, gh = r - token * (int)G;
+    if (mend) {  // values that are not finite, left out where keys were masked, to the queries that see them
+      const int pos = it.ctx + token;
+#pragma unroll 1
+      for (int key = max(it.key_begin, pos - window + 1); key < it.key_end && key <= pos; ++key) {
+        const int page = table[key >> a.shift];
+        if (!there(page)) continue;
+        const uint8_t* vp = a.v + page * a.v_block * kBytes + k_head + (((int64_t)(4 * q) << a.shift) + (key & bs_mask)) * kBytes;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float v = element<T, kFp8>(vp + ((int64_t)(e * kBytes) << a.shift));
+          if (!__builtin_isfinite(v)) sum[e] += v;
+        }
+      }
+    }
     if (it.part >= 0) {
       const int64_t at = ((int64_t)it.part * a.kv_heads + head) * (16 * NC) + r;
       *(f32x4*)(a.acc + at * D + 4 * q) = sum;
       if (q == 0) *(float2*)(a.ml + at * 2) = make_float2(top, total);
       continue;
     }
-    const int token = r / (int)G, gh = r - token * (int)G;
     const float inv = total > 0.0f || total != total ? v_scale / total : 0.0f;
     *(uint2*)(a.out + (int64_t)(it.q_start + token) * a.ot + (int64_t)(head * G + gh) * a.oh + 4 * q) =
         make_uint2(T::pack(sum[0] * inv, sum[1] * inv), T::pack(sum[2] * inv, sum[3] * inv));
@@ -683,11 +735,7 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, uint32_t tile_row
 
 template <class T, int D, bool kFp8>
 kv_status launch_tile(const AttnArgs& a, uint32_t grid, hipStream_t s) {
-  const size_t lds = 2 * (64 * D + D * 64) * 2;
-  static const hipError_t ready = hipFuncSetAttribute((const void*)k_attn_tile<T, D, kFp8>,
-                                                      hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-  KV_HIP(ready);
-  hipLaunchKernelGGL((k_attn_tile<T, D, kFp8>), dim3(grid), dim3(256), lds, s, a);
+  hipLaunchKernelGGL((k_attn_tile<T, D, kFp8>), dim3(grid), dim3(256), 0, s, a);
   KV_HIP(hipGetLastError());
   return KV_OK;
 }
@@ -707,12 +755,15 @@ template <class T, int D, bool kFp8>
 kv_status launch_one(const AttnArgs& a, uint32_t rows, uint32_t grid, hipStream_t s) {
   switch (rows) {
     case 16: return launch_rows<T, D, kFp8, 1>(a, grid, s);
-    case 32: return launch_rows<T, D, kFp8, 2>(a, grid, s);
+    case 32:
+      if constexpr (D <= 128) return launch_rows<T, D, kFp8, 2>(a, grid, s);
+      break;
     case 64:
       if constexpr (D <= 128) return launch_rows<T, D, kFp8, 4>(a, grid, s);
-      [[fallthrough]];
-    default: return launch_tile<T, D, kFp8>(a, grid, s);
+      break;
+    default: break;
   }
+  return launch_tile<T, D, kFp8>(a, grid, s);
 }
 
 template <class T, bool kFp8>

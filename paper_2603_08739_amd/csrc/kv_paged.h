@@ -59,8 +59,8 @@ inline WorkLayout work_layout(const kv_paged_batch& b) {
   w.group = b.q_heads / b.kv_heads;
   const uint64_t most = (uint64_t)(b.max_new ? std::min(b.max_new, b.max_tokens) : b.max_tokens) * w.group;
   const uint32_t busy = std::min(b.n_req, b.max_tokens);
-  // 64 rows of 256 elements from each of four wavefronts would not fit in LDS
-  w.rows = most <= 16 ? 16 : most <= 32 ? 32 : most <= 64 && b.head_dim <= 128 ? 64 : 128;
+  // more than 16 rows of 256 elements are too many registers for one wavefront
+  w.rows = most <= 16 ? 16 : b.head_dim > 128 ? 128 : most <= 32 ? 32 : most <= 64 ? 64 : 128;
   w.max_tiles = w.rows < 128 ? busy : (uint32_t)((uint64_t)b.max_tokens * w.group / 128) + busy;
   // workgroups that the chip holds at a time, a few times over for the small
   // tiles, whose pieces are many and short
