@@ -104,6 +104,7 @@ struct AttnArgs {
   const WorkHeader* head;
   const PieceItem* items;
   const SplitTile* split;
+  uint32_t* done;
   float *acc, *ml;
   float scale;
   uint32_t max_tokens, max_blocks, n_blocks, kv_heads, q_heads, group, window, shift;
@@ -180,6 +181,16 @@ __device__ __forceinline__ void load_to_lds(const uint8_t* from, uint4* to) {
 // A NaN wins: it stays out of the running maximum and reaches the sum as a weight.
 __device__ __forceinline__ float max2(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 __device__ __forceinline__ float max3(float a, float b, float c) { return max2(max2(a, b), c); }
+
+// Partial results pass between workgroups of one kernel, whose second-level caches
+// may differ: stores that go through to where all of them look, loads that look there.
+__device__ __forceinline__ void put_pair(float* p, float x, float y) {
+  const float2 v = make_float2(x, y);
+  __hip_atomic_store((uint64_t*)p, __builtin_bit_cast(uint64_t, v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 get_pair(const float* p) {
+  return __builtin_bit_cast(float2, __hip_atomic_load((const uint64_t*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
 
 // Rescaling is put off until a maximum rises by more than this (base 2): weights
 // then reach 2^8, which their 16-bit types hold with the same relative rounding.
@@ -649,6 +660,14 @@ __global__ __launch_bounds__(256, D * NC <= 128 ? 2 : 1) void k_attn_rows(AttnAr
   mend = mends[0] | mends[1] | mends[2] | mends[3];
   const float v_scale = kFp8 && a.v_scale ? a.v_scale[head] : 1.0f;
   constexpr int kQuads = D / 4;
+  auto put_row = [&](int r, int q, const f32x4& sum, float top, float total) {
+    const int token = r / (int)G, gh = r - token * (int)G;
+    const float inv = total > 0.0f || total != total ? v_scale / total : 0.0f;
+    *(uint2*)(a.out + (int64_t)(it.q_start + token) * a.ot + (int64_t)(head * G + gh) * a.oh + 4 * q) =
+        make_uint2(T::pack(sum[0] * inv, sum[1] * inv), T::pack(sum[2] * inv, sum[3] * inv));
+    if (a.lse && q == 0)
+      a.lse[(int64_t)(it.q_start + token) * a.q_heads + head * G + gh] = (top + __builtin_amdgcn_logf(total)) * kLn2;
+  };
   for (int x = tid; x < rows * kQuads; x += 256) {
     const int r = x / kQuads, q = x % kQuads;
     float top = -__builtin_inff();
@@ -666,9 +685,8 @@ __global__ __launch_bounds__(256, D * NC <= 128 ? 2 : 1) void k_attn_rows(AttnAr
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum[e] = fmaf(f, v[e], sum[e]);
     }
-    const int token = r / (int)G, gh = r - token * (int)G;
     if (mend) {  // values that are not finite, left out where keys were masked, to the queries that see them
-      const int pos = it.ctx + token;
+      const int pos = it.ctx + r / (int)G;
 #pragma unroll 1
       for (int key = max(it.key_begin, pos - window + 1); key < it.key_end && key <= pos; ++key) {
         const int page = table[key >> a.shift];
@@ -683,15 +701,61 @@ __global__ __launch_bounds__(256, D * NC <= 128 ? 2 : 1) void k_attn_rows(AttnAr
     }
     if (it.part >= 0) {
       const int64_t at = ((int64_t)it.part * a.kv_heads + head) * (16 * NC) + r;
-      *(f32x4*)(a.acc + at * D + 4 * q) = sum;
-      if (q == 0) *(float2*)(a.ml + at * 2) = make_float2(top, total);
+      put_pair(a.acc + at * D + 4 * q, sum[0], sum[1]);
+      put_pair(a.acc + at * D + 4 * q + 2, sum[2], sum[3]);
+      if (q == 0) put_pair(a.ml + at * 2, top, total);
       continue;
     }
-    const float inv = total > 0.0f || total != total ? v_scale / total : 0.0f;
-    *(uint2*)(a.out + (int64_t)(it.q_start + token) * a.ot + (int64_t)(head * G + gh) * a.oh + 4 * q) =
-        make_uint2(T::pack(sum[0] * inv, sum[1] * inv), T::pack(sum[2] * inv, sum[3] * inv));
-    if (a.lse && q == 0)
-      a.lse[(int64_t)(it.q_start + token) * a.q_heads + head * G + gh] = (top + __builtin_amdgcn_logf(total)) * kLn2;
+    put_row(r, q, sum, top, total);
+  }
+  if (it.part < 0) return;
+
+  // The last of the tile's workgroups joins its pieces, in their order.
+  __shared__ int last;
+  // Every wavefront waits until its own stores, which went through, are done.  (A
+  // release and an acquire fence for the device would do it for plain stores, but they
+  // write back and invalidate whole caches: single tokens of 64 chats took 290 us
+  // with them, 130 without.)
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  uint32_t* done = a.done + (uint32_t)it.split * a.kv_heads + head;
+  if (tid == 0) last = __hip_atomic_fetch_add(done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)it.n_parts - 1;
+  __syncthreads();
+  if (!last) return;
+  if (tid == 0) __hip_atomic_store(done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  const int64_t step = (int64_t)a.kv_heads * 16 * NC;
+  for (int x = tid; x < rows * kQuads; x += 256) {
+    const int r = x / kQuads, q = x % kQuads;
+    const int64_t at = ((int64_t)it.first_part * a.kv_heads + head) * (16 * NC) + r;
+    const float* ml = a.ml + at * 2;
+    const float* acc = a.acc + at * D + 4 * q;
+    f32x4 sum{};
+    float top = -__builtin_inff(), total = 0.0f;
+    constexpr int kBatch = NC == 4 ? 2 : 4;  // pieces read at a time
+    for (int i = 0; i < it.n_parts; i += kBatch) {
+      float2 st[kBatch], lo[kBatch], hi[kBatch];
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const int64_t p = min(i + j, it.n_parts - 1) * step;
+        st[j] = get_pair(ml + p * 2);
+        lo[j] = get_pair(acc + p * D);
+        hi[j] = get_pair(acc + p * D + 2);
+      }
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        if (i + j >= it.n_parts) break;
+        const float m_new = fmaxf(top, st[j].x);
+        const float sub = m_new == -__builtin_inff() ? 0.0f : m_new;
+        const float was = __builtin_amdgcn_exp2f(top - sub), is = __builtin_amdgcn_exp2f(st[j].x - sub);
+        top = m_new;
+        total = fmaf(is, st[j].y, total * was);
+        sum[0] = fmaf(is, lo[j].x, sum[0] * was);
+        sum[1] = fmaf(is, lo[j].y, sum[1] * was);
+        sum[2] = fmaf(is, hi[j].x, sum[2] * was);
+        sum[3] = fmaf(is, hi[j].y, sum[3] * was);
+      }
+    }
+    put_row(r, q, sum, top, total);
   }
 }
 
@@ -790,6 +854,7 @@ kv_status paged_attention(const kv_paged_batch& b, const WorkLayout& w, const kv
   a.head = (const WorkHeader*)at;
   a.items = (const PieceItem*)(at + w.items);
   a.split = (const SplitTile*)(at + w.split);
+  a.done = (uint32_t*)((uint8_t*)b.work + w.done);
   a.acc = (float*)((uint8_t*)b.work + w.acc), a.ml = (float*)((uint8_t*)b.work + w.ml);
   a.scale = scale;
   a.max_tokens = b.max_tokens, a.max_blocks = b.max_blocks, a.n_blocks = c.n_blocks;
@@ -806,9 +871,11 @@ kv_status paged_attention(const kv_paged_batch& b, const WorkLayout& w, const kv
     st = fp8 ? launch_dim<F16, true>(a, b.head_dim, w.rows, (uint32_t)grid, s)
              : launch_dim<F16, false>(a, b.head_dim, w.rows, (uint32_t)grid, s);
   if (st != KV_OK) return st;
-  // no tile can be cut when the whole table is at most one piece long
+  // tiles of few rows are joined already, and none is cut when the whole table is
+  // at most one piece long
+  if (w.rows < 128) return KV_OK;
   if ((uint64_t)b.max_blocks * b.block_size <= kMinUnits * kKeyUnit) return KV_OK;
-  const dim3 join(w.max_split * b.kv_heads, w.rows < 128 ? 1 : 4);
+  const dim3 join(w.max_split * b.kv_heads, 4);
   if (dtype == KV_DT_BF16)
     hipLaunchKernelGGL(k_attn_join<BF16>, join, dim3(256), 0, s, a, w.rows, b.head_dim, (uint32_t)fp8);
   else

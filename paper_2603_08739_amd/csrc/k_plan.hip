@@ -24,6 +24,7 @@ struct PlanArgs {
   WorkHeader* head;
   PieceItem* items;
   SplitTile* split;
+  uint32_t* done;
 };
 
 // Tiles are numbered request by request, a request's last rows first: they see
@@ -219,10 +220,16 @@ __global__ __launch_bounds__(kNT) void k_paged_plan(PlanArgs a) {
       it.key_begin = x.key_begin + (int32_t)((uint64_t)x.units * i / cut) * (int32_t)kKeyUnit;
       it.key_end = min(x.key_end, x.key_begin + (int32_t)((uint64_t)x.units * (i + 1) / cut) * (int32_t)kKeyUnit);
       it.part = cut > 1 ? (int32_t)min(part_at + i, a.max_parts - 1) : -1;
+      it.split = (int32_t)min(split_at, a.max_split - 1);
+      it.first_part = (int32_t)part_at;
+      it.n_parts = (int32_t)cut;
+      it.pad = 0;
       a.items[at + i] = it;
     }
     n_items += s0, n_split += s1, n_parts += s2;
   }
+  const uint32_t counters = min(n_split, a.max_split) * a.b.kv_heads;
+  for (uint32_t i = tid; i < counters; i += kNT) a.done[i] = 0;
   if (tid == 0) {
     a.head->n_items = (int32_t)min(n_items, a.max_items);
     a.head->n_split = (int32_t)min(n_split, a.max_split);
@@ -241,6 +248,7 @@ kv_status paged_plan(const kv_paged_batch& b, const WorkLayout& w, hipStream_t s
   a.head = (WorkHeader*)at;
   a.items = (PieceItem*)(at + w.items);
   a.split = (SplitTile*)(at + w.split);
+  a.done = (uint32_t*)(at + w.done);
   const uint32_t grid = 1 + (b.max_tokens + kTokensEach - 1) / kTokensEach;
   // three arrays of n_req and two ends: at most 49 KB
   hipLaunchKernelGGL(k_paged_plan, dim3(grid), dim3(kNT), (3 * b.n_req + 2) * sizeof(int32_t), s, a);

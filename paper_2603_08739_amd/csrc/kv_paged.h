@@ -15,8 +15,9 @@ namespace kv {
 // the G query heads that read the head, token by token (row = token * G +
 // head).  A tile is up to `rows` of them; a piece is a tile over a range of
 // keys.  Long tiles are cut into pieces so that the chip is filled and no
-// workgroup runs much longer than the others; the pieces of one tile are
-// joined by a second kernel.
+// workgroup runs much longer than the others.  The pieces of a tile of few rows are
+// joined by the workgroup that finishes last (`done` counts them per tile and
+// head, and is 0 between calls), those of 128 rows by a second kernel.
 constexpr uint32_t kKeyUnit = 64;  // key ranges of pieces are cut at multiples of this
 
 struct PieceItem {
@@ -28,6 +29,9 @@ struct PieceItem {
   int32_t key_begin;  // multiple of kKeyUnit
   int32_t key_end;
   int32_t part;       // partial result to write, or -1: the tile's only piece
+  int32_t split;      // the tile's place among the cut ones
+  int32_t first_part, n_parts;
+  int32_t pad;
 };
 
 struct SplitTile {
@@ -47,7 +51,7 @@ struct WorkLayout {
   uint32_t max_tiles;
   uint32_t pieces;     // pieces wanted per key/value head
   uint32_t max_items, max_parts, max_split;
-  uint64_t items, split, acc, ml, bytes;  // offsets from work; bytes in all
+  uint64_t items, split, done, acc, ml, bytes;  // offsets from work; bytes in all
 };
 
 // A piece is no shorter than this many units: below it, the joining of partial
@@ -64,7 +68,7 @@ inline WorkLayout work_layout(const kv_paged_batch& b) {
   w.max_tiles = w.rows < 128 ? busy : (uint32_t)((uint64_t)b.max_tokens * w.group / 128) + busy;
   // workgroups that the chip holds at a time, a few times over for the small
   // tiles, whose pieces are many and short
-  const uint32_t target = w.rows < 128 ? 2048 : 512;
+  const uint32_t target = w.rows < 128 ? 1536 : 1024;
   w.pieces = (target + b.kv_heads - 1) / b.kv_heads;
   w.max_items = w.max_tiles + w.pieces;
   w.max_parts = 2 * w.pieces;
@@ -72,7 +76,8 @@ inline WorkLayout work_layout(const kv_paged_batch& b) {
   auto up = [](uint64_t x) { return (x + 255) / 256 * 256; };
   w.items = sizeof(WorkHeader);
   w.split = up(w.items + (uint64_t)w.max_items * sizeof(PieceItem));
-  w.acc = up(w.split + (uint64_t)w.max_split * sizeof(SplitTile));
+  w.done = up(w.split + (uint64_t)w.max_split * sizeof(SplitTile));
+  w.acc = up(w.done + (uint64_t)w.max_split * b.kv_heads * sizeof(uint32_t));
   const uint64_t rows = (uint64_t)w.max_parts * b.kv_heads * w.rows;
   w.ml = up(w.acc + rows * b.head_dim * sizeof(float));
   w.bytes = up(w.ml + rows * 2 * sizeof(float));
