@@ -203,8 +203,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attn_tile(AttnArgs a)
   __shared__ uint4 k_lds0[L::kChunks], k_lds1[L::kChunks], v_lds0[L::kChunks], v_lds1[L::kChunks];
   __shared__ int mend;
   const uint32_t item = blockIdx.x / a.kv_heads, head = blockIdx.x % a.kv_heads;
+  const PieceItem it = a.items[item];  // loaded whether there is one or not: one wait for both
   if ((int)item >= a.head->n_items) return;
-  const PieceItem it = a.items[item];
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
   const int col = lane & 31, half = lane >> 5;
   const uint32_t G = a.group;
@@ -462,8 +462,8 @@ __global__ __launch_bounds__(256, D * NC <= 128 ? 2 : 1) void k_attn_rows(AttnAr
   constexpr int kPer = kFp8 ? 16 : 8, kKeys = 4 * kPer, kBlocks = kKeys / 16, kSteps = kKeys / 32;
   constexpr int kLoadsK = D / 4 / kPer;  // 16-byte loads of a key row by a lane
   const uint32_t item = blockIdx.x / a.kv_heads, head = blockIdx.x % a.kv_heads;
+  const PieceItem it = a.items[item];  // loaded whether there is one or not: one wait for both
   if ((int)item >= a.head->n_items) return;
-  const PieceItem it = a.items[item];
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
   const int col = lane & 15, g = lane >> 4;
   const uint32_t G = a.group;
@@ -723,39 +723,61 @@ __global__ __launch_bounds__(256, D * NC <= 128 ? 2 : 1) void k_attn_rows(AttnAr
   __syncthreads();
   if (!last) return;
   if (tid == 0) __hip_atomic_store(done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  // the pieces' weights first, in the memory of the wavefronts' results
+  float* weight = flds;                      // [rows][kMaxParts]
+  float* sums = flds + 16 * NC * kMaxParts;  // [rows][2]
   const int64_t step = (int64_t)a.kv_heads * 16 * NC;
+  const int64_t part0 = ((int64_t)it.first_part * a.kv_heads + head) * (16 * NC);
+  for (int x = tid; x < rows * 8; x += 256) {  // 8 lanes a row
+    const int r = x / 8, j = x % 8;
+    float2 st[kMaxParts / 8];
+#pragma unroll
+    for (int i = 0; i < kMaxParts / 8; ++i)
+      if (8 * i < it.n_parts) st[i] = get_pair(a.ml + (part0 + r + min(8 * i + j, it.n_parts - 1) * step) * 2);
+    float top = -__builtin_inff(), total = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kMaxParts / 8; ++i)
+      if (8 * i + j < it.n_parts) top = fmaxf(top, st[i].x);
+#pragma unroll
+    for (int d = 1; d < 8; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 8));
+    const float sub = top == -__builtin_inff() ? 0.0f : top;
+#pragma unroll
+    for (int i = 0; i < kMaxParts / 8; ++i)
+      if (8 * i + j < it.n_parts) {
+        const float f = __builtin_amdgcn_exp2f(st[i].x - sub);
+        weight[r * kMaxParts + 8 * i + j] = f;
+        total = fmaf(f, st[i].y, total);
+      }
+#pragma unroll
+    for (int d = 1; d < 8; d <<= 1) total += __shfl_xor(total, d, 8);
+    if (j == 0) sums[2 * r] = top, sums[2 * r + 1] = total;
+  }
+  __syncthreads();
   for (int x = tid; x < rows * kQuads; x += 256) {
     const int r = x / kQuads, q = x % kQuads;
-    const int64_t at = ((int64_t)it.first_part * a.kv_heads + head) * (16 * NC) + r;
-    const float* ml = a.ml + at * 2;
-    const float* acc = a.acc + at * D + 4 * q;
+    const float* acc = a.acc + (part0 + r) * D + 4 * q;
     f32x4 sum{};
-    float top = -__builtin_inff(), total = 0.0f;
-    constexpr int kBatch = NC == 4 ? 2 : 4;  // pieces read at a time
+    constexpr int kBatch = NC == 1 ? 8 : 2;  // pieces read at a time
+#pragma unroll 1
     for (int i = 0; i < it.n_parts; i += kBatch) {
-      float2 st[kBatch], lo[kBatch], hi[kBatch];
+      float2 lo[kBatch], hi[kBatch];
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
-        const int64_t p = min(i + j, it.n_parts - 1) * step;
-        st[j] = get_pair(ml + p * 2);
-        lo[j] = get_pair(acc + p * D);
-        hi[j] = get_pair(acc + p * D + 2);
+        const float* p = acc + min(i + j, it.n_parts - 1) * step * D;
+        lo[j] = get_pair(p);
+        hi[j] = get_pair(p + 2);
       }
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
         if (i + j >= it.n_parts) break;
-        const float m_new = fmaxf(top, st[j].x);
-        const float sub = m_new == -__builtin_inff() ? 0.0f : m_new;
-        const float was = __builtin_amdgcn_exp2f(top - sub), is = __builtin_amdgcn_exp2f(st[j].x - sub);
-        top = m_new;
-        total = fmaf(is, st[j].y, total * was);
-        sum[0] = fmaf(is, lo[j].x, sum[0] * was);
-        sum[1] = fmaf(is, lo[j].y, sum[1] * was);
-        sum[2] = fmaf(is, hi[j].x, sum[2] * was);
-        sum[3] = fmaf(is, hi[j].y, sum[3] * was);
+        const float f = weight[r * kMaxParts + i + j];
+        sum[0] = fmaf(f, lo[j].x, sum[0]);
+        sum[1] = fmaf(f, lo[j].y, sum[1]);
+        sum[2] = fmaf(f, hi[j].x, sum[2]);
+        sum[3] = fmaf(f, hi[j].y, sum[3]);
       }
     }
-    put_row(r, q, sum, top, total);
+    put_row(r, q, sum, sums[2 * r], sums[2 * r + 1]);
   }
 }
 
@@ -823,7 +845,7 @@ kv_status launch_one(const AttnArgs& a, uint32_t rows, uint32_t grid, hipStream_
       if constexpr (D <= 128) return launch_rows<T, D, kFp8, 2>(a, grid, s);
       break;
     case 64:
-      if constexpr (D <= 128) return launch_rows<T, D, kFp8, 4>(a, grid, s);
+      if constexpr (D <= 64) return launch_rows<T, D, kFp8, 4>(a, grid, s);
       break;
     default: break;
   }

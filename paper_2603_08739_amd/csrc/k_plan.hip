@@ -4,7 +4,7 @@
 // One launch: every workgroup works out the requests' first tokens and first
 // new blocks for itself (two prefix sums over at most 4,096 requests, kept in
 // LDS), so none waits for another.  Workgroup 0 writes the per-request arrays
-// and the work list, the others 2,048 tokens each; a token finds its request
+// and the work list, the others four tokens a thread; a token finds its request
 // by binary search, and the token at the start of a new block enters the block
 // in the table.  Whole numbers throughout; bound by latency (the chain of
 // loads, sums and stores of one workgroup) up to some 10^5 tokens.
@@ -14,8 +14,6 @@
 namespace kv {
 namespace {
 
-constexpr int kNT = 256;
-constexpr uint32_t kTokensEach = 2048;
 
 struct PlanArgs {
   kv_paged_batch b;
@@ -31,6 +29,13 @@ struct PlanArgs {
 // the most keys, and the longest pieces should start first.
 struct Tile {
   int32_t req, row0, row_end, key_begin, key_end, units;
+};
+
+// A tile, its first piece's place among those of its batch, and where its partial
+// results go.
+struct Cut {
+  Tile x;
+  uint32_t at, cut, split_at, part_at;
 };
 
 __device__ __forceinline__ Tile tile_of(const PlanArgs& a, const int32_t* first_tile, const int32_t* start,
@@ -57,12 +62,14 @@ __device__ __forceinline__ Tile tile_of(const PlanArgs& a, const int32_t* first_
   return x;
 }
 
+template <int kNT>
 __global__ __launch_bounds__(kNT) void k_paged_plan(PlanArgs a) {
+  constexpr uint32_t kTokensEach = 4 * kNT;
   // start: first token of each request; ctx: its cached tokens (0 where its
   // lengths are refused); fresh: its first new block's place in the free list
   // (workgroup 0: then its first tile)
   extern __shared__ int32_t lds[];
-  __shared__ uint32_t sh[2 * kNT / 64 + 2];
+  __shared__ uint32_t sh[2][2 * kNT / 64];  // taken in turn by the sums, which then need one barrier each
   const uint32_t R = a.b.n_req, T = a.b.max_tokens, bs = a.b.block_size;
   int32_t* start = lds;
   int32_t* ctx = start + R + 1;
@@ -85,7 +92,7 @@ __global__ __launch_bounds__(kNT) void k_paged_plan(PlanArgs a) {
       }
     }
     uint32_t sum;
-    const uint32_t before = block_excl_scan_u32<kNT>((uint32_t)n, sh, sum);
+    const uint32_t before = block_excl_scan_u32<kNT, false>((uint32_t)n, sh[0], sum);
     const uint32_t at = tokens + before;
     if (at + n > T) {
       flags |= KV_PLAN_TOKENS;
@@ -98,7 +105,7 @@ __global__ __launch_bounds__(kNT) void k_paged_plan(PlanArgs a) {
     }
     const uint32_t need = r < R ? (uint32_t)((c + n + bs - 1) >> a.shift) - (uint32_t)((c + bs - 1) >> a.shift) : 0u;
     uint32_t total;
-    const uint32_t place = block_excl_scan_u32<kNT>(need, sh, total);
+    const uint32_t place = block_excl_scan_u32<kNT, false>(need, sh[1], total);
     if (r < R) fresh[r] = (int32_t)(blocks + place);
     tokens += sum;
     blocks += total;
@@ -172,7 +179,7 @@ __global__ __launch_bounds__(kNT) void k_paged_plan(PlanArgs a) {
     const uint32_t r = r0 + tid;
     const uint32_t rows = r < R ? (uint32_t)(start[r + 1] - start[r]) * a.group : 0u;
     uint32_t sum;
-    const uint32_t before = block_excl_scan_u32<kNT>((rows + a.rows - 1) / a.rows, sh, sum);
+    const uint32_t before = block_excl_scan_u32<kNT, false>((rows + a.rows - 1) / a.rows, sh[(r0 / kNT) & 1], sum);
     if (r < R) first_tile[r] = (int32_t)(n_tiles + before);
     n_tiles += sum;
   }
@@ -183,23 +190,29 @@ __global__ __launch_bounds__(kNT) void k_paged_plan(PlanArgs a) {
   if (tid == 0) total_units = 0;
   __syncthreads();
   unsigned long long mine = 0;
-  for (uint32_t t = tid; t < n_tiles; t += kNT) mine += (unsigned)tile_of(a, first_tile, start, ctx, (int32_t)t).units;
+  Tile x{};
+  for (uint32_t t = tid; t < n_tiles; t += kNT) {
+    x = tile_of(a, first_tile, start, ctx, (int32_t)t);
+    mine += (uint32_t)x.units;
+  }
   if (mine) atomicAdd(&total_units, mine);
   __syncthreads();
   const uint32_t longest = max(kMinUnits, (uint32_t)((total_units + a.pieces - 1) / a.pieces));
+  // kNT tiles at a time; their pieces are shared out among all threads
+  __shared__ Cut cuts[kNT];
   uint32_t n_items = 0, n_split = 0, n_parts = 0;
   for (uint32_t t0 = 0; t0 < n_tiles; t0 += kNT) {
     const uint32_t t = t0 + tid;
-    Tile x{};
     uint32_t cut = 0;
     if (t < n_tiles) {
-      x = tile_of(a, first_tile, start, ctx, (int32_t)t);
-      cut = ((uint32_t)x.units + longest - 1) / longest;
+      if (n_tiles > (uint32_t)kNT) x = tile_of(a, first_tile, start, ctx, (int32_t)t);
+      cut = min(((uint32_t)x.units + longest - 1) / longest, (uint32_t)kMaxParts);
     }
     uint32_t at, split_at, s0, s1, s2;
-    block_excl_scan2_u32<kNT>(cut, cut > 1 ? 1u : 0u, sh, at, split_at, s0, s1);
-    uint32_t part_at = block_excl_scan_u32<kNT>(cut > 1 ? cut : 0u, sh, s2);
-    at += n_items, split_at += n_split, part_at += n_parts;
+    block_excl_scan2_u32<kNT, false>(cut, cut > 1 ? 1u : 0u, sh[0], at, split_at, s0, s1);
+    const uint32_t part_at = n_parts + block_excl_scan_u32<kNT, false>(cut > 1 ? cut : 0u, sh[1], s2);
+    split_at += n_split;
+    cuts[tid] = Cut{x, at, cut, split_at, part_at};
     if (cut > 1 && split_at < a.max_split) {
       SplitTile y{};
       y.q_start = start[x.req];
@@ -209,24 +222,37 @@ __global__ __launch_bounds__(kNT) void k_paged_plan(PlanArgs a) {
       y.n_parts = (int32_t)cut;
       a.split[split_at] = y;
     }
-    for (uint32_t i = 0; i < cut && at + i < a.max_items; ++i) {
+    __syncthreads();
+    for (uint32_t k = tid; k < s0 && n_items + k < a.max_items; k += kNT) {
+      int lo = 0, hi = kNT;  // cuts[lo].at <= k, and the first of those after it is beyond k
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (cuts[mid].at <= k)
+          lo = mid;
+        else
+          hi = mid;
+      }
+      const Cut c = cuts[lo];
+      // equal pieces: the first `more` are one unit longer
+      const uint32_t i = k - c.at, each = (uint32_t)c.x.units / c.cut, more = (uint32_t)c.x.units % c.cut;
+      const uint32_t from = i * each + min(i, more), to = from + each + (i < more ? 1u : 0u);
       PieceItem it;
-      it.req = x.req;
-      it.q_start = start[x.req];
-      it.ctx = ctx[x.req];
-      it.row_end = x.row_end;
-      it.row0 = x.row0;
-      // equal pieces
-      it.key_begin = x.key_begin + (int32_t)((uint64_t)x.units * i / cut) * (int32_t)kKeyUnit;
-      it.key_end = min(x.key_end, x.key_begin + (int32_t)((uint64_t)x.units * (i + 1) / cut) * (int32_t)kKeyUnit);
-      it.part = cut > 1 ? (int32_t)min(part_at + i, a.max_parts - 1) : -1;
-      it.split = (int32_t)min(split_at, a.max_split - 1);
-      it.first_part = (int32_t)part_at;
-      it.n_parts = (int32_t)cut;
+      it.req = c.x.req;
+      it.q_start = start[c.x.req];
+      it.ctx = ctx[c.x.req];
+      it.row_end = c.x.row_end;
+      it.row0 = c.x.row0;
+      it.key_begin = c.x.key_begin + (int32_t)(from * kKeyUnit);
+      it.key_end = min(c.x.key_end, c.x.key_begin + (int32_t)(to * kKeyUnit));
+      it.part = c.cut > 1 ? (int32_t)min(c.part_at + i, a.max_parts - 1) : -1;
+      it.split = (int32_t)min(c.split_at, a.max_split - 1);
+      it.first_part = (int32_t)c.part_at;
+      it.n_parts = (int32_t)c.cut;
       it.pad = 0;
-      a.items[at + i] = it;
+      a.items[n_items + k] = it;
     }
     n_items += s0, n_split += s1, n_parts += s2;
+    __syncthreads();  // cuts
   }
   const uint32_t counters = min(n_split, a.max_split) * a.b.kv_heads;
   for (uint32_t i = tid; i < counters; i += kNT) a.done[i] = 0;
@@ -249,9 +275,17 @@ kv_status paged_plan(const kv_paged_batch& b, const WorkLayout& w, hipStream_t s
   a.items = (PieceItem*)(at + w.items);
   a.split = (SplitTile*)(at + w.split);
   a.done = (uint32_t*)(at + w.done);
-  const uint32_t grid = 1 + (b.max_tokens + kTokensEach - 1) / kTokensEach;
+  // Threads of a workgroup: few requests and tiles are done in one round of 256, whose
+  // barriers are the cheaper ones (a step of 64 chats: 7.4 us a call, 8.8 with 1,024
+  // threads); more of them need the threads (1,000 ragged prompts: 15.6 us, 26.7 with 256).
+  const uint32_t threads = b.n_req <= 256 && w.max_tiles <= 512 ? 256 : 1024;
+  const uint32_t grid = 1 + (b.max_tokens + 4 * threads - 1) / (4 * threads);
   // three arrays of n_req and two ends: at most 49 KB
-  hipLaunchKernelGGL(k_paged_plan, dim3(grid), dim3(kNT), (3 * b.n_req + 2) * sizeof(int32_t), s, a);
+  const size_t lds = (3 * b.n_req + 2) * sizeof(int32_t);
+  if (threads == 256)
+    hipLaunchKernelGGL(k_paged_plan<256>, dim3(grid), dim3(256), lds, s, a);
+  else
+    hipLaunchKernelGGL(k_paged_plan<1024>, dim3(grid), dim3(1024), lds, s, a);
   KV_HIP(hipGetLastError());
   return KV_OK;
 }

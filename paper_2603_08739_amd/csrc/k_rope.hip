@@ -190,11 +190,9 @@ struct AppendArgs {
 };
 
 // Queries and keys: threads as in k_rope_apply, groups of query heads before
-// groups of key heads.  Values: a thread takes 8 elements of a head.  Where the
-// tokens from t on fill 8 neighbouring places of a block, the thread of the first
-// of them turns an 8 x 8 square in registers and writes 16-byte rows of the
-// transposed block (8-byte ones in 8 bits); tokens outside such a run are
-// written element by element.
+// groups of key heads.  Values: a workgroup turns 64 tokens by 64 elements of a head
+// in LDS; then lanes are tokens, so that tokens in neighbouring places of a block are
+// written side by side, whatever request and place they begin at.
 template <class V, bool kHalf, bool kFp8>
 __global__ __launch_bounds__(256) void k_append(AppendArgs a) {
   const uint32_t n_tokens = min((uint32_t)max(a.q_start[a.n_req], 0), a.max_tokens);
@@ -262,71 +260,38 @@ __global__ __launch_bounds__(256) void k_append(AppendArgs a) {
     return;
   }
 
-  const uint64_t id = (uint64_t)(blockIdx.x - a.qk_blocks) * 256 + threadIdx.x;
-  const uint32_t chunks = a.dim / 8;
-  const uint32_t chunk = (uint32_t)(id % chunks);
-  const uint64_t rest = id / chunks;
-  const uint32_t h = (uint32_t)(rest % a.kv_heads);
-  const uint64_t token = rest / a.kv_heads;
-  if (token >= n_tokens) return;
-  const int64_t slot = a.slot[token];
-  if (slot < 0 || (uint64_t)slot >= a.slots) return;
-  // the run of 8 places this one lies in, if the neighbouring tokens fill it
-  const int64_t run = slot & 7;
-  bool whole = (int64_t)token >= run && token - run + 8 <= n_tokens;
-  if (whole) {
-    const int64_t* s = a.slot + (token - run);
+  const uint32_t strips = a.dim / 64;
+  const uint32_t id = blockIdx.x - a.qk_blocks, strip = id % strips, h = id / strips % a.kv_heads;
+  const uint32_t t0 = id / strips / a.kv_heads * 64;
+  __shared__ uint16_t tile[64][66];  // 33 words a row: a column's reads fall on different banks
 #pragma unroll
-    for (int i = 0; i < 8; ++i) whole = whole && s[i] == slot - run + i;
-  }
-  if (whole && run) return;
-  const float s = kFp8 && a.v_scale ? a.v_scale[h] : 1.0f;
-  const uint16_t* x = a.v + (int64_t)token * a.vt + h * a.vh + chunk * 8;
-  const int64_t at = (slot >> a.block_shift) * a.v_block +
-                     (((int64_t)h * a.dim + chunk * 8) << a.block_shift) + (slot & block_mask);
-  if (whole) {
-    uint4 row[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) row[i] = *(const uint4*)(x + i * a.vt);
-    if (kFp8) {
-      float f[8][8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) unpack<V>(row[i], f[i]);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float col[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) col[i] = f[i][e] / s;
-        *(uint2*)((uint8_t*)a.vc + at + ((int64_t)e << a.block_shift)) = pack_fp8(col);
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        uint32_t col[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t p = ((const uint32_t*)&row[2 * i])[e / 2], q = ((const uint32_t*)&row[2 * i + 1])[e / 2];
-          col[i] = e & 1 ? (p >> 16) | (q & 0xffff0000u) : (p & 0xffffu) | (q << 16);
-        }
-        *(uint4*)((uint16_t*)a.vc + at + ((int64_t)e << a.block_shift)) = make_uint4(col[0], col[1], col[2], col[3]);
-      }
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t t = threadIdx.x / 8 + 32 * i, chunk = threadIdx.x % 8;
+    if (t0 + t < n_tokens) {
+      const uint4 u = *(const uint4*)(a.v + (int64_t)(t0 + t) * a.vt + h * a.vh + strip * 64 + chunk * 8);
+      uint32_t* to = (uint32_t*)&tile[t][chunk * 8];
+      to[0] = u.x, to[1] = u.y, to[2] = u.z, to[3] = u.w;
     }
-    return;
   }
-  const uint4 u = *(const uint4*)x;
-  if (kFp8) {
-    float f[8];
-    unpack<V>(u, f);
+  const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int64_t slot = t0 + lane < n_tokens ? a.slot[t0 + lane] : -1;
+  __syncthreads();
+  if (slot < 0 || (uint64_t)slot >= a.slots) return;
+  const int64_t at = (slot >> a.block_shift) * a.v_block +
+                     (((int64_t)h * a.dim + strip * 64 + wave * 16) << a.block_shift) + (slot & block_mask);
+  const float s = kFp8 && a.v_scale ? a.v_scale[h] : 1.0f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = f[e] / s;
-    const uint2 w = pack_fp8(f);
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      ((uint8_t*)a.vc)[at + ((int64_t)e << a.block_shift)] = (uint8_t)((e < 4 ? w.x : w.y) >> (8 * (e & 3)));
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      ((uint16_t*)a.vc)[at + ((int64_t)e << a.block_shift)] = (uint16_t)(((const uint32_t*)&u)[e / 2] >> (16 * (e & 1)));
+  for (int d = 0; d < 16; d += 2) {
+    const uint32_t two = *(const uint32_t*)&tile[lane][wave * 16 + d];
+    if (kFp8) {
+      const V v = __builtin_bit_cast(V, make_uint4(two, 0, 0, 0));
+      const uint32_t w = pack_fp8x4((float)v[0] / s, (float)v[1] / s, 0.0f, 0.0f);
+      ((uint8_t*)a.vc)[at + ((int64_t)d << a.block_shift)] = (uint8_t)w;
+      ((uint8_t*)a.vc)[at + ((int64_t)(d + 1) << a.block_shift)] = (uint8_t)(w >> 8);
+    } else {
+      ((uint16_t*)a.vc)[at + ((int64_t)d << a.block_shift)] = (uint16_t)two;
+      ((uint16_t*)a.vc)[at + ((int64_t)(d + 1) << a.block_shift)] = (uint16_t)(two >> 16);
+    }
   }
 }
 
@@ -409,7 +374,7 @@ kv_status paged_append(const kv_paged_batch& b, const kv_paged_cache& c, const R
   a.groups = a.q_groups + (b.kv_heads + a.heads_each - 1) / a.heads_each;
   a.block_shift = (uint32_t)__builtin_ctz(b.block_size);
   const uint64_t qk = ((uint64_t)b.max_tokens * a.groups * a.units + 255) / 256;
-  const uint64_t vv = ((uint64_t)b.max_tokens * b.kv_heads * (b.head_dim / 8) + 255) / 256;
+  const uint64_t vv = ((uint64_t)b.max_tokens + 63) / 64 * b.kv_heads * (b.head_dim / 64);
   if (qk + vv > 0x7fffffffull) return fail(KV_ERR_UNSUPPORTED, "kv_paged_append: too many heads for one call");
   a.qk_blocks = (uint32_t)qk;
   const bool half = !r || r->layout == KV_ROPE_HALF, fp8 = c.dtype == KV_DT_FP8;

@@ -57,14 +57,20 @@ struct WorkLayout {
 // A piece is no shorter than this many units: below it, the joining of partial
 // results costs more than the shorter walk saves.
 constexpr uint32_t kMinUnits = 4;
+// A tile is cut into no more pieces than this: one workgroup reads them all.  (One
+// context of 131,072 tokens, 8 key/value heads of 128: 101 us with 32 pieces a head,
+// 105 with 64, 130 with 192.)
+constexpr int kMaxParts = 32;
 
 inline WorkLayout work_layout(const kv_paged_batch& b) {
   WorkLayout w{};
   w.group = b.q_heads / b.kv_heads;
   const uint64_t most = (uint64_t)(b.max_new ? std::min(b.max_new, b.max_tokens) : b.max_tokens) * w.group;
   const uint32_t busy = std::min(b.n_req, b.max_tokens);
-  // more than 16 rows of 256 elements are too many registers for one wavefront
-  w.rows = most <= 16 ? 16 : b.head_dim > 128 ? 128 : most <= 32 ? 32 : most <= 64 ? 64 : 128;
+  // rows * head_dim is at most 4,096 in the kernel for few rows: a wavefront holds
+  // the whole tile's results, and more would not leave room for its loads
+  const uint32_t few = most <= 16 ? 16 : most <= 32 ? 32 : 64;
+  w.rows = most <= 64 && few * b.head_dim <= 4096 ? few : 128;
   w.max_tiles = w.rows < 128 ? busy : (uint32_t)((uint64_t)b.max_tokens * w.group / 128) + busy;
   // workgroups that the chip holds at a time, a few times over for the small
   // tiles, whose pieces are many and short

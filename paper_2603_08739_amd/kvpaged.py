@@ -13,7 +13,9 @@ from __future__ import annotations
 
 import ctypes
 
-from .kvcfg import KV_ERR_INVALID, KV_ERR_UNSUPPORTED, KV_OK, LIB, KvError, _check, _stream  # noqa: F401
+import torch
+
+from .kvcfg import KV_ERR_INVALID, KV_ERR_UNSUPPORTED, KV_OK, LIB, KvError, _check, kv_last_error  # noqa: F401
 
 KV_DT_BF16, KV_DT_F16, KV_DT_FP8 = 0, 1, 2
 KV_ROPE_HALF, KV_ROPE_INTERLEAVED = 0, 1
@@ -66,13 +68,17 @@ for _name in EXPORTS:
     getattr(LIB, _name).restype = ctypes.c_int
 
 
-def _types():
-    import torch
-    return {torch.bfloat16: KV_DT_BF16, torch.float16: KV_DT_F16, torch.float8_e4m3fn: KV_DT_FP8}
-
-
-_TYPES = _types()
+_TYPES = {torch.bfloat16: KV_DT_BF16, torch.float16: KV_DT_F16, torch.float8_e4m3fn: KV_DT_FP8}
 _NO_VIEW = kv_heads_view()
+
+
+def _stream(stream):
+    """The stream's handle; None is the current stream of the current device.  These
+    calls take a few microseconds on the device, and torch.cuda.current_stream()
+    would take three more: the handle is asked for without making a Stream."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return stream if isinstance(stream, int) else stream.cuda_stream
 
 
 def _dtype(t, name):
@@ -132,7 +138,6 @@ class Rope:
 def kv_rope_apply(rope: Rope, x, pos, out=None, backward=False, stream=None):
     """x: [tokens, heads, dim] bfloat16 / float16 at any token and head stride;
     pos: int32 [tokens]; out: like x (may be x), made when None.  Returns out."""
-    import torch
     n, heads, dim = x.shape
     if out is None:
         out = torch.empty((n, heads, dim), dtype=x.dtype, device=x.device)
@@ -151,7 +156,6 @@ class Plan:
 
     def __init__(self, n_req, max_tokens, block_size, max_blocks, q_heads, kv_heads, head_dim,
                  max_new=None, window=0, device="cuda"):
-        import torch
         b = self.batch = kv_paged_batch()
         b.n_req, b.max_tokens, b.max_new = int(n_req), int(max_tokens), int(max_new or 0)
         b.block_size, b.max_blocks = int(block_size), int(max_blocks)
@@ -174,7 +178,6 @@ class Plan:
 def kv_paged_plan(plan: Plan, ctx_len, new_len, table, free_list=None, stream=None):
     """ctx_len, new_len: int32 [n_req]; table: int32 [n_req, max_blocks], written
     where a request takes new blocks from free_list (int32), read otherwise."""
-    import torch
     b = plan.batch
     if table.dim() != 2 or table.shape[1] != b.max_blocks:
         raise ValueError(f"table has shape {tuple(table.shape)}; the plan's rows have {b.max_blocks} blocks")
@@ -195,7 +198,6 @@ class Cache:
     contiguous.  float8_e4m3fn caches take k_scale, v_scale: float32 [kv_heads]."""
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
-        import torch
         if k.dim() != 4 or v.dim() != 4 or not k.is_cuda or not v.is_cuda:
             raise ValueError("k and v must be CUDA tensors of four dimensions")
         n, heads, block, dim = k.shape
@@ -244,7 +246,6 @@ def kv_paged_append(plan: Plan, cache: Cache, k, v, q=None, q_out=None, rope: Ro
 def kv_paged_attention(plan: Plan, cache: Cache, q, out=None, lse=None, scale=None, stream=None):
     """q, out: [>=max_tokens, q_heads, dim]; lse: float32 [>=max_tokens, q_heads] or
     None; scale: dim ** -0.5 when None.  Returns out."""
-    import torch
     b = _fits(plan, cache)
     n, heads, dim = b.max_tokens, b.q_heads, b.head_dim
     if out is None:
