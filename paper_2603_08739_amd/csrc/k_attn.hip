@@ -313,9 +313,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attn_tile(AttnArgs a)
   };
 
   int pages = look_up(it.key_begin), next_pages = look_up(it.key_begin + BK);
-  auto step = [&](int key, const uint4* lk, uint4* lv, uint4* next_k, uint4* next_v) __attribute__((always_inline)) {
-    // groups of 16 keys that are there
-    const uint32_t valid = (uint32_t)__ballot(there(pages) && key + 16 * (lane & 3) < it.key_end) & 15u;
+  uint32_t valid = 0;  // groups of 16 keys that are there
+  auto arrive = [&](int key, uint4* lv, uint4* next_k, uint4* next_v) __attribute__((always_inline)) {
+    valid = (uint32_t)__ballot(there(pages) && key + 16 * (lane & 3) < it.key_end) & 15u;
     // This wavefront's loads to LDS have arrived.  They are counted with the loads
     // from memory, which the barrier itself does not wait for.
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -324,7 +324,11 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attn_tile(AttnArgs a)
     if (key + BK < it.key_end) fetch(key + BK, next_pages, next_k, next_v);
     pages = next_pages;
     next_pages = look_up(key + 2 * BK);
-    if (!wave_on || key > last_pos || key + BK <= first_pos - window + 1) return;
+  };
+  auto active = [&](int key) {
+    return wave_on && key < it.key_end && key <= last_pos && key + BK > first_pos - window + 1;
+  };
+  auto multiply = [&](int key, const uint4* lk, const uint4* lv) __attribute__((always_inline)) {
     const bool edge = key + BK - 1 > first_pos || key <= last_pos - window || valid != 15;
     f32x16 s[2];
 #pragma unroll
@@ -343,15 +347,15 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attn_tile(AttnArgs a)
       }
     }
     if (edge) {
+      constexpr int kRun = kFp8 ? 16 : 8;
+      const int from = key + kRun * half, most = qpos - from, least = qpos - window - from;
 #pragma unroll
       for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          constexpr int kRun = kFp8 ? 16 : 8;
           const int at = 32 * n + (kFp8 ? e : 16 * (e >> 3) + (e & 7));  // + kRun * half: the key
-          const int from = key + kRun * half;
           const bool here = (valid >> (2 * n + (kFp8 ? half : e >> 3))) & 1;
-          s[n][e] = here && at <= qpos - from && at > qpos - window - from ? s[n][e] : -__builtin_inff();
+          s[n][e] = (here & (at <= most) & (at > least)) ? s[n][e] : -__builtin_inff();
         }
     }
     float top = max3(s[0][0], s[0][1], s[1][0]);
@@ -396,9 +400,13 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attn_tile(AttnArgs a)
   if (tid == 0) mend = 0;
   fetch(it.key_begin, pages, k_lds0, v_lds0);
   __syncthreads();  // mend
+  // two tiles a turn: their places in LDS are known to the compiler, which waits for
+  // loads to LDS before any read that they might concern
   for (int key = it.key_begin; key < it.key_end; key += 2 * BK) {
-    step(key, k_lds0, v_lds0, k_lds1, v_lds1);
-    if (key + BK < it.key_end) step(key + BK, k_lds1, v_lds1, k_lds0, v_lds0);
+    arrive(key, v_lds0, k_lds1, v_lds1);
+    if (active(key)) multiply(key, k_lds0, v_lds0);
+    arrive(key + BK, v_lds1, k_lds0, v_lds0);
+    if (active(key + BK)) multiply(key + BK, k_lds1, v_lds1);
   }
   // What was taken out, added to what has been stored for this lane's query (an
   // infinity or a NaN decides its element whatever the scale).
