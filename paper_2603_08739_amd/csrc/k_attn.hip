@@ -19,7 +19,7 @@
 //                 through LDS: chunks of prompts, bound by the matrix cores
 //   k_attn_rows   up to 64 rows (single tokens): keys and values go from memory
 //                 to registers, four wavefronts share the keys; bound by memory
-//   k_attn_join   the pieces of tiles whose keys were cut
+//   k_attn_join   the pieces of tiles of 128 rows whose keys were cut
 //
 // A weight of 0 times a NaN or an infinity in a masked value would be NaN.  Where
 // a tile holds masked keys, values are therefore looked at: non-finite ones are
@@ -358,12 +358,14 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attn_tile(AttnArgs a)
           s[n][e] = (here & (at <= most) & (at > least)) ? s[n][e] : -__builtin_inff();
         }
     }
-    float top = max3(s[0][0], s[0][1], s[1][0]);
+    float tops[4];  // four chains: one of 16 would be all latency
 #pragma unroll
-    for (int e = 2; e < 16; e += 2) top = max3(top, s[0][e], s[0][e + 1]);
+    for (int x = 0; x < 4; ++x) {
+      tops[x] = max3(s[x >> 1][8 * (x & 1)], s[x >> 1][8 * (x & 1) + 1], s[x >> 1][8 * (x & 1) + 2]);
 #pragma unroll
-    for (int e = 1; e < 15; e += 2) top = max3(top, s[1][e], s[1][e + 1]);
-    top = max2(top, s[1][15]);
+      for (int e = 3; e < 7; e += 2) tops[x] = max3(tops[x], s[x >> 1][8 * (x & 1) + e], s[x >> 1][8 * (x & 1) + e + 1]);
+    }
+    float top = max3(max3(tops[0], s[0][7], tops[1]), max3(tops[2], s[0][15], tops[3]), max2(s[1][7], s[1][15]));
     top = max2(top, other_half(top)) * c;
     if (__any(top > m + kSlack)) {
       const float m_new = fmaxf(m, top);
@@ -789,41 +791,42 @@ __global__ __launch_bounds__(256, D * NC <= 128 ? 2 : 1) void k_attn_rows(AttnAr
   }
 }
 
-// Joins the pieces of a tile: rows of one (tile, head) by blockIdx, 4 elements
-// a thread.
+// Joins the pieces of tiles of 128 rows, 4 elements a thread.  A row of a tile and
+// head takes dim / 4 threads; workgroups walk over the rows of all cut tiles.
 template <class T>
-__global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, uint32_t tile_rows, uint32_t dim, uint32_t fp8) {
-  const uint32_t tile = blockIdx.x / a.kv_heads, head = blockIdx.x % a.kv_heads;
-  if ((int)tile >= a.head->n_split) return;
-  const SplitTile t = a.split[tile];
-  const uint32_t quads = dim / 4;
-  const float v_scale = fp8 && a.v_scale ? a.v_scale[head] : 1.0f;
-  const uint32_t rows = (uint32_t)min((int)tile_rows, t.row_end - t.row0);
-  for (uint32_t x = blockIdx.y * 256 + threadIdx.x; x < rows * quads; x += gridDim.y * 256) {
-    const uint32_t r = x / quads, q = x % quads;
-    float top = -__builtin_inff();
-    for (int i = 0; i < t.n_parts; ++i)
-      top = fmaxf(top, a.ml[(((int64_t)(t.first_part + i) * a.kv_heads + head) * tile_rows + r) * 2]);
+__global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, uint32_t dim, uint32_t fp8) {
+  const uint32_t quads = dim / 4, each = 256 / quads;  // rows of a workgroup
+  const uint32_t q = threadIdx.x % quads, chunks = 128 / each;
+  const uint32_t total = (uint32_t)a.head->n_split * a.kv_heads * chunks;
+  for (uint32_t w = blockIdx.x; w < total; w += gridDim.x) {
+    const uint32_t r = w % chunks * each + threadIdx.x / quads, head = w / chunks % a.kv_heads;
+    const SplitTile t = a.split[w / chunks / a.kv_heads];
+    const int row = t.row0 + (int)r;
+    if (row >= t.row_end) continue;
+    const int64_t step = (int64_t)a.kv_heads * 128, at = ((int64_t)t.first_part * a.kv_heads + head) * 128 + r;
+    const float* ml = a.ml + at * 2;
+    const float* acc = a.acc + at * dim + 4 * q;
+    float top = -__builtin_inff(), total_l = 0.0f;
+    for (int i = 0; i < t.n_parts; ++i) top = fmaxf(top, ml[i * step * 2]);
     const float sub = top == -__builtin_inff() ? 0.0f : top;
     f32x4 sum{};
-    float total = 0.0f;
+#pragma unroll 4
     for (int i = 0; i < t.n_parts; ++i) {
-      const int64_t at = ((int64_t)(t.first_part + i) * a.kv_heads + head) * tile_rows + r;
-      const float2 ml = *(const float2*)(a.ml + at * 2);
-      const float f = __builtin_amdgcn_exp2f(ml.x - sub);
-      const f32x4 v = *(const f32x4*)(a.acc + at * dim + 4 * q);
-      total = fmaf(f, ml.y, total);
+      const float2 st = *(const float2*)(ml + i * step * 2);
+      const f32x4 v = *(const f32x4*)(acc + i * step * dim);
+      const float f = __builtin_amdgcn_exp2f(st.x - sub);
+      total_l = fmaf(f, st.y, total_l);
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum[e] = fmaf(f, v[e], sum[e]);
     }
-    const int row = t.row0 + (int)r;
     const int token = row / (int)a.group, gh = row - token * (int)a.group;
-    const float inv = total > 0.0f || total != total ? v_scale / total : 0.0f;
+    const float v_scale = fp8 && a.v_scale ? a.v_scale[head] : 1.0f;
+    const float inv = total_l > 0.0f || total_l != total_l ? v_scale / total_l : 0.0f;
     *(uint2*)(a.out + (int64_t)(t.q_start + token) * a.ot + (int64_t)(head * a.group + gh) * a.oh + 4 * q) =
         make_uint2(T::pack(sum[0] * inv, sum[1] * inv), T::pack(sum[2] * inv, sum[3] * inv));
     if (a.lse && q == 0)
       a.lse[(int64_t)(t.q_start + token) * a.q_heads + head * a.group + gh] =
-          (top + __builtin_amdgcn_logf(total)) * kLn2;
+          (top + __builtin_amdgcn_logf(total_l)) * kLn2;
   }
 }
 
@@ -905,11 +908,11 @@ kv_status paged_attention(const kv_paged_batch& b, const WorkLayout& w, const kv
   // at most one piece long
   if (w.rows < 128) return KV_OK;
   if ((uint64_t)b.max_blocks * b.block_size <= kMinUnits * kKeyUnit) return KV_OK;
-  const dim3 join(w.max_split * b.kv_heads, 4);
+  const dim3 join(std::min<uint32_t>(w.max_split * b.kv_heads * 4, 4096));
   if (dtype == KV_DT_BF16)
-    hipLaunchKernelGGL(k_attn_join<BF16>, join, dim3(256), 0, s, a, w.rows, b.head_dim, (uint32_t)fp8);
+    hipLaunchKernelGGL(k_attn_join<BF16>, join, dim3(256), 0, s, a, b.head_dim, (uint32_t)fp8);
   else
-    hipLaunchKernelGGL(k_attn_join<F16>, join, dim3(256), 0, s, a, w.rows, b.head_dim, (uint32_t)fp8);
+    hipLaunchKernelGGL(k_attn_join<F16>, join, dim3(256), 0, s, a, b.head_dim, (uint32_t)fp8);
   KV_HIP(hipGetLastError());
   return KV_OK;
 }
