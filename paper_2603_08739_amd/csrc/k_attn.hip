@@ -43,6 +43,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
 struct BF16 {
+  static constexpr float kWeights = 1.0e12f;  // of 32 keys: far from overflow
   static constexpr uint32_t kExp = 0x7f80u;  // exponent bits: all set = not finite
   static __device__ __forceinline__ float value(uint16_t u) { return (float)__builtin_bit_cast(__bf16, u); }
   static __device__ __forceinline__ f32x16 mfma32(const uint4& a, const uint4& b, const f32x16& c) {
@@ -65,6 +66,7 @@ struct BF16 {
 };
 
 struct F16 {
+  static constexpr float kWeights = 16384.0f;  // none of them overflows to infinity
   static constexpr uint32_t kExp = 0x7c00u;
   static __device__ __forceinline__ float value(uint16_t u) { return (float)__builtin_bit_cast(_Float16, u); }
   static __device__ __forceinline__ f32x16 mfma32(const uint4& a, const uint4& b, const f32x16& c) {
@@ -210,16 +212,17 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attn_tile(AttnArgs a)
   const uint32_t G = a.group;
 
   // this lane's query
-  const int row = it.row0 + 32 * wave + col;
-  const int safe_row = min(row, it.row_end - 1);
-  const int token = safe_row / (int)G, gh = safe_row - token * (int)G;
-  const int qpos = it.ctx + token;
+  int end_lane = lane;
+  asm volatile("" : "+v"(end_lane));
+  const int row = min(it.row0 + 32 * wave + col, it.row_end - 1);
+  const int qpos = it.ctx + row / (int)G;
   const bool wave_on = it.row0 + 32 * wave < it.row_end;
   // Operand step s of the first product: elements 16*s + 8*half + 0..7 of a 16-bit
   // cache; of an 8-bit one, whose 16-byte chunk serves two steps, 32*(s/2) + 16*half
   // + 8*(s%2) + 0..7
   uint4 qf[D / 16];
   {
+    const int token = row / (int)G, gh = row - token * (int)G;
     const uint16_t* p = a.q + (int64_t)(it.q_start + token) * a.qt + (int64_t)(head * G + gh) * a.qh;
 #pragma unroll
     for (int s = 0; s < D / 16; ++s)
@@ -330,69 +333,83 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attn_tile(AttnArgs a)
   };
   auto multiply = [&](int key, const uint4* lk, const uint4* lv) __attribute__((always_inline)) {
     const bool edge = key + BK - 1 > first_pos || key <= last_pos - window || valid != 15;
+    // Weights are taken from the maximum of the keys seen when it was last looked for
+    // (at first, and again when a weight has grown past kWeights: their sum, at
+    // hand anyway, says so; the tile is then done again).  Their rounding is relative,
+    // so that costs no accuracy, and the maximum of every tile, 16 instructions
+    // and a wait across lanes, is saved: a prompt of 8,111 tokens 601 -> 580 us.  Heads of
+    // 256 have no registers to spare for the way back and look at every tile.
+    constexpr bool kLazy = D <= 128;
     f32x16 s[2];
+    uint4 p[4];
+    bool look = !kLazy || __any(m == -__builtin_inff());
+    for (;;) {
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      s[n] = f32x16{};
-      if (kFp8) {
+      for (int n = 0; n < 2; ++n) {
+        s[n] = f32x16{};
+        if (kFp8) {
 #pragma unroll
-        for (int d = 0; d < D / 32; ++d) {
-          const uint4 u = lk[L::k_at(32 * n + krow, 2 * d + half)];
-          s[n] = T::mfma32(widen8<T>(u.x, u.y), qf[2 * d], s[n]);
-          s[n] = T::mfma32(widen8<T>(u.z, u.w), qf[2 * d + 1], s[n]);
+          for (int d = 0; d < D / 32; ++d) {
+            const uint4 u = lk[L::k_at(32 * n + krow, 2 * d + half)];
+            s[n] = T::mfma32(widen8<T>(u.x, u.y), qf[2 * d], s[n]);
+            s[n] = T::mfma32(widen8<T>(u.z, u.w), qf[2 * d + 1], s[n]);
+          }
+        } else {
+#pragma unroll
+          for (int d = 0; d < D / 16; ++d) s[n] = T::mfma32(lk[L::k_at(32 * n + krow, 2 * d + half)], qf[d], s[n]);
         }
-      } else {
-#pragma unroll
-        for (int d = 0; d < D / 16; ++d) s[n] = T::mfma32(lk[L::k_at(32 * n + krow, 2 * d + half)], qf[d], s[n]);
       }
-    }
-    if (edge) {
-      constexpr int kRun = kFp8 ? 16 : 8;
-      const int from = key + kRun * half, most = qpos - from, least = qpos - window - from;
+      if (edge) {
+        constexpr int kRun = kFp8 ? 16 : 8;
+        const int from = key + kRun * half, most = qpos - from, least = qpos - window - from;
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int at = 32 * n + (kFp8 ? e : 16 * (e >> 3) + (e & 7));  // + kRun * half: the key
+            const bool here = (valid >> (2 * n + (kFp8 ? half : e >> 3))) & 1;
+            s[n][e] = (here & (at <= most) & (at > least)) ? s[n][e] : -__builtin_inff();
+          }
+      }
+      if (look) {
+        float top = s[0][0];
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int e = 0; e < 16; e += 2) top = max3(top, s[n][e], s[n][e + 1]);
+        top = max2(top, other_half(top)) * c;
+        if (kLazy || __any(top > m + kSlack)) {
+          const float m_new = fmaxf(m, top);
+          const float alpha = m_new == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
+          m = m_new;
+          l *= alpha;
+#pragma unroll
+          for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[i][e] *= alpha;
+        }
+      }
+      const float sub = m == -__builtin_inff() ? 0.0f : m;
+      float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const int at = 32 * n + (kFp8 ? e : 16 * (e >> 3) + (e & 7));  // + kRun * half: the key
-          const bool here = (valid >> (2 * n + (kFp8 ? half : e >> 3))) & 1;
-          s[n][e] = (here & (at <= most) & (at > least)) ? s[n][e] : -__builtin_inff();
+          s[n][e] = __builtin_amdgcn_exp2f(fmaf(s[n][e], c, -sub));
+          sum[e & 3] += s[n][e];
         }
-    }
-    float tops[4];  // four chains: one of 16 would be all latency
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      tops[x] = max3(s[x >> 1][8 * (x & 1)], s[x >> 1][8 * (x & 1) + 1], s[x >> 1][8 * (x & 1) + 2]);
-#pragma unroll
-      for (int e = 3; e < 7; e += 2) tops[x] = max3(tops[x], s[x >> 1][8 * (x & 1) + e], s[x >> 1][8 * (x & 1) + e + 1]);
-    }
-    float top = max3(max3(tops[0], s[0][7], tops[1]), max3(tops[2], s[0][15], tops[3]), max2(s[1][7], s[1][15]));
-    top = max2(top, other_half(top)) * c;
-    if (__any(top > m + kSlack)) {
-      const float m_new = fmaxf(m, top);
-      const float alpha = m_new == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
-      m = m_new;
-      l *= alpha;
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[i][e] *= alpha;
-    }
-    const float sub = m == -__builtin_inff() ? 0.0f : m;
-    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    uint4 p[4];
-#pragma unroll
-    for (int n = 0; n < 2; ++n) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        s[n][e] = __builtin_amdgcn_exp2f(fmaf(s[n][e], c, -sub));
-        sum[e & 3] += s[n][e];
+        for (int h = 0; h < 2; ++h)
+          p[2 * n + h] = make_uint4(T::pack(s[n][8 * h], s[n][8 * h + 1]), T::pack(s[n][8 * h + 2], s[n][8 * h + 3]),
+                                    T::pack(s[n][8 * h + 4], s[n][8 * h + 5]), T::pack(s[n][8 * h + 6], s[n][8 * h + 7]));
       }
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        p[2 * n + h] = make_uint4(T::pack(s[n][8 * h], s[n][8 * h + 1]), T::pack(s[n][8 * h + 2], s[n][8 * h + 3]),
-                                  T::pack(s[n][8 * h + 4], s[n][8 * h + 5]), T::pack(s[n][8 * h + 6], s[n][8 * h + 7]));
+      const float all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      if (!kLazy || look || !__any(!(all <= T::kWeights))) {
+        l += all;
+        break;
+      }
+      look = true;
     }
-    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
@@ -430,7 +447,11 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attn_tile(AttnArgs a)
   __syncthreads();
   const bool mended = mend != 0;
   l += other_half(l);
-  if (row >= it.row_end) return;
+  // the query again, from a copy of the lane: kept through the loop, its numbers would
+  // take registers
+  const int last_row = it.row0 + 32 * wave + (end_lane & 31);
+  if (last_row >= it.row_end) return;
+  const int token = last_row / (int)G, gh = last_row - token * (int)G;
   if (it.part >= 0) {
     const int64_t at = ((int64_t)it.part * a.kv_heads + head) * 128 + 32 * wave + col;
     float* acc = a.acc + at * D;

@@ -8,9 +8,9 @@ import pytest
 pytestmark = pytest.mark.gpu
 
 
-def case(ctx, new, block, heads, dim, dtype, kept, window=0, drop=(), max_new=None, pad=0, spare=3, edit=None, scale=None, seed=0):
+def case(ctx, new, block, heads, dim, dtype, kept, window=0, drop=(), max_new=None, pad=0, spare=3, edit=None, edit_q=None, scale=None, seed=0):
     """Runs one batch and checks it; drop: (request, column) entries set to -1; edit(kc,
-    vc, table) changes the cache before the call."""
+    vc, table) and edit_q(q) change the inputs before the call."""
     import torch
     from oracle import paged as O
     from paper_2603_08739_amd import kvpaged as K
@@ -26,6 +26,8 @@ def case(ctx, new, block, heads, dim, dtype, kept, window=0, drop=(), max_new=No
     total = sum(new)
     T = total + pad
     q = (torch.randn(T, H, dim, generator=gen) * (1 + torch.rand(H, 1, generator=gen))).to(TYPES[dtype]).cuda()
+    if edit_q:
+        edit_q(q)
     p = K.Plan(len(ctx), T, block, table.shape[1], H, J, dim, max_new=max_new, window=window)
     i32 = dict(dtype=torch.int32, device="cuda")
     K.kv_paged_plan(p, torch.tensor(ctx, **i32), torch.tensor(new, **i32), table)
@@ -141,6 +143,29 @@ def test_large_scores():
     case([200, 0, 64], [1, 1, 1], 16, (8, 2), 128, "bf16", "bf16", edit=edit, max_new=1)
     case([200, 0, 64], [70, 3, 20], 16, (8, 2), 128, "bf16", "bf16", edit=edit)
     case([200, 0, 64], [70, 3, 20], 16, (8, 2), 64, "f16", "f16", scale=0.01)
+
+
+@pytest.mark.parametrize("dtype, kept", KINDS)
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("step", [0.02, 0.3, 4.0])
+def test_rising_scores(dtype, kept, dim, step):
+    """Every key's score is above that of the one before it, by little or by so much
+    that weights taken from an earlier maximum would overflow."""
+    import torch
+
+    def edit(kc, vc, table):
+        k = torch.zeros(kc.shape, device="cuda")
+        for row in table.tolist():
+            for i, page in enumerate(row):
+                if page >= 0:  # element 0 carries the score: q[0] is 8 below
+                    k[page, :, :, 0] = (step * torch.arange(16 * i, 16 * i + 16, device="cuda")).clamp(max=440.0)
+        kc.copy_(k.to(kc.dtype))
+
+    def queries(q):
+        q.mul_(0.25)[..., 0] = 8.0
+
+    case([150, 0, 3], [90, 200, 1], 16, (4, 2), dim, dtype, kept, edit=edit, edit_q=queries, scale=0.25)
+    case([150, 0, 300], [1, 1, 1], 16, (4, 2), dim, dtype, kept, edit=edit, edit_q=queries, scale=0.25, max_new=1)
 
 
 @pytest.mark.parametrize("ctx, new, heads, dim, kept, max_new", [
