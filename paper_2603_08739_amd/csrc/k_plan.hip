@@ -15,6 +15,8 @@ namespace kv {
 namespace {
 
 
+constexpr uint32_t kClasses = 64;  // of piece lengths: one for each lane of a wavefront
+
 struct PlanArgs {
   kv_paged_batch b;
   uint32_t shift;  // log2 of block_size
@@ -25,8 +27,7 @@ struct PlanArgs {
   uint32_t* done;
 };
 
-// Tiles are numbered request by request, a request's last rows first: they see
-// the most keys, and the longest pieces should start first.
+// Tiles are numbered request by request, a request's last rows first.
 struct Tile {
   int32_t req, row0, row_end, key_begin, key_end, units;
 };
@@ -187,73 +188,115 @@ __global__ __launch_bounds__(kNT) void k_paged_plan(PlanArgs a) {
   __syncthreads();
   // how long a piece may be
   __shared__ unsigned long long total_units;
-  if (tid == 0) total_units = 0;
+  __shared__ uint32_t most_units, in_class[kClasses];
+  if (tid == 0) total_units = 0, most_units = 0;
+  if (tid < kClasses) in_class[tid] = 0;
   __syncthreads();
+  // each thread keeps its first tiles: finding one is a search
+  constexpr uint32_t kKeep = 2;
+  Tile kept[kKeep]{};
+  auto tile_at = [&](uint32_t t) { return tile_of(a, first_tile, start, ctx, (int32_t)t); };
+  auto each_tile = [&](auto&& f) {
+#pragma unroll
+    for (uint32_t i = 0; i < kKeep; ++i)
+      if (tid + i * kNT < n_tiles) f(kept[i]);
+    for (uint32_t t = tid + kKeep * kNT; t < n_tiles; t += kNT) f(tile_at(t));
+  };
+#pragma unroll
+  for (uint32_t i = 0; i < kKeep; ++i)
+    if (tid + i * kNT < n_tiles) kept[i] = tile_at(tid + i * kNT);
   unsigned long long mine = 0;
-  Tile x{};
-  for (uint32_t t = tid; t < n_tiles; t += kNT) {
-    x = tile_of(a, first_tile, start, ctx, (int32_t)t);
-    mine += (uint32_t)x.units;
-  }
-  if (mine) atomicAdd(&total_units, mine);
+  uint32_t most = 0;
+  each_tile([&](const Tile& y) {
+    mine += (uint32_t)y.units;
+    most = max(most, (uint32_t)y.units);
+  });
+  mine = wave_sum(mine);
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, d, 64));
+  if (lane_id() == 0 && mine) atomicAdd(&total_units, mine), atomicMax(&most_units, most);
   __syncthreads();
   const uint32_t longest = max(kMinUnits, (uint32_t)((total_units + a.pieces - 1) / a.pieces));
-  // kNT tiles at a time; their pieces are shared out among all threads
-  __shared__ Cut cuts[kNT];
-  uint32_t n_items = 0, n_split = 0, n_parts = 0;
-  for (uint32_t t0 = 0; t0 < n_tiles; t0 += kNT) {
-    const uint32_t t = t0 + tid;
-    uint32_t cut = 0;
-    if (t < n_tiles) {
-      if (n_tiles > (uint32_t)kNT) x = tile_of(a, first_tile, start, ctx, (int32_t)t);
-      cut = min(((uint32_t)x.units + longest - 1) / longest, (uint32_t)kMaxParts);
-    }
-    uint32_t at, split_at, s0, s1, s2;
-    block_excl_scan2_u32<kNT, false>(cut, cut > 1 ? 1u : 0u, sh[0], at, split_at, s0, s1);
-    const uint32_t part_at = n_parts + block_excl_scan_u32<kNT, false>(cut > 1 ? cut : 0u, sh[1], s2);
-    split_at += n_split;
-    cuts[tid] = Cut{x, at, cut, split_at, part_at};
-    if (cut > 1 && split_at < a.max_split) {
-      SplitTile y{};
-      y.q_start = start[x.req];
-      y.row_end = x.row_end;
-      y.row0 = x.row0;
-      y.first_part = (int32_t)part_at;
-      y.n_parts = (int32_t)cut;
-      a.split[split_at] = y;
-    }
-    __syncthreads();
-    for (uint32_t k = tid; k < s0 && n_items + k < a.max_items; k += kNT) {
-      int lo = 0, hi = kNT;  // cuts[lo].at <= k, and the first of those after it is beyond k
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (cuts[mid].at <= k)
-          lo = mid;
-        else
-          hi = mid;
-      }
-      const Cut c = cuts[lo];
-      // equal pieces: the first `more` are one unit longer
-      const uint32_t i = k - c.at, each = (uint32_t)c.x.units / c.cut, more = (uint32_t)c.x.units % c.cut;
-      const uint32_t from = i * each + min(i, more), to = from + each + (i < more ? 1u : 0u);
-      PieceItem it;
-      it.req = c.x.req;
-      it.q_start = start[c.x.req];
-      it.ctx = ctx[c.x.req];
-      it.row_end = c.x.row_end;
-      it.row0 = c.x.row0;
-      it.key_begin = c.x.key_begin + (int32_t)(from * kKeyUnit);
-      it.key_end = min(c.x.key_end, c.x.key_begin + (int32_t)(to * kKeyUnit));
-      it.part = c.cut > 1 ? (int32_t)min(c.part_at + i, a.max_parts - 1) : -1;
-      it.split = (int32_t)min(c.split_at, a.max_split - 1);
-      it.first_part = (int32_t)c.part_at;
-      it.n_parts = (int32_t)c.cut;
-      it.pad = 0;
-      a.items[n_items + k] = it;
-    }
-    n_items += s0, n_split += s1, n_parts += s2;
-    __syncthreads();  // cuts
+  auto cut_of = [&](const Tile& y) { return min(((uint32_t)y.units + longest - 1) / longest, (uint32_t)kMaxParts); };
+  // Long pieces go first, so that the last ones to end are short: the list is ordered
+  // by classes of length (within one, in any order: results do not depend on it).
+  uint32_t shift = 0;
+  while ((max(longest, most_units / kMaxParts + 1) >> shift) >= kClasses) ++shift;
+  auto class_of = [&](uint32_t units) { return kClasses - 1 - min(units >> shift, kClasses - 1); };
+  each_tile([&](const Tile& y) {
+    const uint32_t cut = cut_of(y), each = (uint32_t)y.units / cut, more = (uint32_t)y.units % cut;
+    if (more) atomicAdd(&in_class[class_of(each + 1)], more);
+    atomicAdd(&in_class[class_of(each)], cut - more);
+  });
+  __syncthreads();
+  uint32_t n_items = 0;
+  if (tid < 64) {
+    const uint32_t n = in_class[tid], upto = wave_incl_scan_u32(n);
+    in_class[tid] = upto - n;  // then: where the class's next piece goes
+    n_items = (uint32_t)__shfl((int)upto, 63, 64);
   }
+  __syncthreads();
+  // kNT tiles at a time: a thread writes its tile where it is one piece; the pieces of
+  // those that are cut are shared out among all threads
+  __shared__ Cut cuts[kNT];
+  auto put = [&](const Cut& c, uint32_t i) {
+    // equal pieces: the first `more` are one unit longer
+    const uint32_t each = (uint32_t)c.x.units / c.cut, more = (uint32_t)c.x.units % c.cut;
+    const uint32_t from = i * each + min(i, more), last = from + each + (i < more ? 1u : 0u);
+    PieceItem it;
+    it.req = c.x.req;
+    it.q_start = start[c.x.req];
+    it.ctx = ctx[c.x.req];
+    it.row_end = c.x.row_end;
+    it.row0 = c.x.row0;
+    it.key_begin = c.x.key_begin + (int32_t)(from * kKeyUnit);
+    it.key_end = min(c.x.key_end, c.x.key_begin + (int32_t)(last * kKeyUnit));
+    it.part = c.cut > 1 ? (int32_t)min(c.part_at + i, a.max_parts - 1) : -1;
+    it.split = (int32_t)min(c.split_at, a.max_split - 1);
+    it.first_part = (int32_t)c.part_at;
+    it.n_parts = (int32_t)c.cut;
+    it.pad = 0;
+    const uint32_t to = atomicAdd(&in_class[class_of(last - from)], 1u);
+    if (to < a.max_items) a.items[to] = it;
+  };
+  uint32_t n_split = 0, n_parts = 0;
+  auto batch = [&](uint32_t t0, const Tile& y) {
+    const uint32_t cut = t0 + tid < n_tiles ? cut_of(y) : 0u;
+    uint32_t at, split_at, parts, splits;
+    block_excl_scan2_u32<kNT, false>(cut > 1 ? cut : 0u, cut > 1 ? 1u : 0u, sh[(t0 / kNT) & 1], at, split_at, parts, splits);
+    const Cut c{y, at, cut, n_split + split_at, n_parts + at};
+    if (cut == 1) put(c, 0);
+    if (parts) {
+      cuts[tid] = c;
+      if (cut > 1 && c.split_at < a.max_split) {
+        SplitTile z{};
+        z.q_start = start[y.req];
+        z.row_end = y.row_end;
+        z.row0 = y.row0;
+        z.first_part = (int32_t)c.part_at;
+        z.n_parts = (int32_t)cut;
+        a.split[c.split_at] = z;
+      }
+      __syncthreads();
+      for (uint32_t k = tid; k < parts; k += kNT) {
+        int lo = 0, hi = kNT;  // the last cut tile whose first piece is not after k
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) / 2;
+          if (cuts[mid].at <= k)
+            lo = mid;
+          else
+            hi = mid;
+        }
+        put(cuts[lo], k - cuts[lo].at);
+      }
+      __syncthreads();  // cuts
+    }
+    n_split += splits, n_parts += parts;
+  };
+#pragma unroll
+  for (uint32_t i = 0; i < kKeep; ++i)
+    if (i * kNT < n_tiles) batch(i * kNT, kept[i]);
+  for (uint32_t t0 = kKeep * kNT; t0 < n_tiles; t0 += kNT) batch(t0, t0 + tid < n_tiles ? tile_at(t0 + tid) : Tile{});
   const uint32_t counters = min(n_split, a.max_split) * a.b.kv_heads;
   for (uint32_t i = tid; i < counters; i += kNT) a.done[i] = 0;
   if (tid == 0) {
