@@ -211,7 +211,8 @@ kv_status kv_paged_append(const kv_paged_batch* b, const kv_paged_cache* c, cons
  *   lse       device float [max_tokens][q_heads] or NULL
  *   scale     > 0 and finite
  * Rows past the step's last token are left alone.  The batch must have been
- * planned on this stream (or waited for) with the same sizes, window included. */
+ * planned on this stream (or waited for) with the same sizes, window included:
+ * with a work list for other sizes the call writes nothing. */
 kv_status kv_paged_attention(const kv_paged_batch* b, const kv_paged_cache* c, uint32_t dtype,
                              kv_heads_view q, kv_heads_view out, float* lse, float scale,
                              void* stream);

@@ -24,7 +24,7 @@
 // A weight of 0 times a NaN or an infinity in a masked value would be NaN.  Where
 // a tile holds masked keys, values are therefore looked at: non-finite ones are
 // taken out of the product and added back only to the queries that see them.
-#include <type_traits>
+#include <atomic>
 
 #include "kv_device.h"
 #include "kv_paged.h"
@@ -103,6 +103,7 @@ struct AttnArgs {
   int64_t k_block, v_block;  // bytes
   const float *k_scale, *v_scale;
   const int32_t* table;
+  uint64_t sizes;
   const WorkHeader* head;
   const PieceItem* items;
   const SplitTile* split;
@@ -206,7 +207,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attn_tile(AttnArgs a)
   __shared__ int mend;
   const uint32_t item = blockIdx.x / a.kv_heads, head = blockIdx.x % a.kv_heads;
   const PieceItem it = a.items[item];  // loaded whether there is one or not: one wait for both
-  if ((int)item >= a.head->n_items) return;
+  if ((int)item >= a.head->n_items || a.head->sizes != a.sizes) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
   const int col = lane & 31, half = lane >> 5;
   const uint32_t G = a.group;
@@ -322,7 +323,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attn_tile(AttnArgs a)
     // This wavefront's loads to LDS have arrived.  They are counted with the loads
     // from memory, which the barrier itself does not wait for.
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    clean(key, valid, lv);
+    if (key < it.key_end) clean(key, valid, lv);
     __syncthreads();  // everybody's have, and nobody reads the other keys any more
     if (key + BK < it.key_end) fetch(key + BK, next_pages, next_k, next_v);
     pages = next_pages;
@@ -494,7 +495,7 @@ __global__ __launch_bounds__(256, D * NC <= 128 ? 2 : 1) void k_attn_rows(AttnAr
   constexpr int kLoadsK = D / 4 / kPer;  // 16-byte loads of a key row by a lane
   const uint32_t item = blockIdx.x / a.kv_heads, head = blockIdx.x % a.kv_heads;
   const PieceItem it = a.items[item];  // loaded whether there is one or not: one wait for both
-  if ((int)item >= a.head->n_items) return;
+  if ((int)item >= a.head->n_items || a.head->sizes != a.sizes) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
   const int col = lane & 15, g = lane >> 4;
   const uint32_t G = a.group;
@@ -754,11 +755,23 @@ __global__ __launch_bounds__(256, D * NC <= 128 ? 2 : 1) void k_attn_rows(AttnAr
   __syncthreads();
   if (!last) return;
   if (tid == 0) __hip_atomic_store(done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  // the pieces' weights first, in the memory of the wavefronts' results
-  float* weight = flds;                      // [rows][kMaxParts]
-  float* sums = flds + 16 * NC * kMaxParts;  // [rows][2]
   const int64_t step = (int64_t)a.kv_heads * 16 * NC;
   const int64_t part0 = ((int64_t)it.first_part * a.kv_heads + head) * (16 * NC);
+  constexpr int kBatch = NC == 1 ? 8 : 2;  // pieces read at a time
+  float2 lo[kBatch], hi[kBatch];
+  auto read = [&](int x, int i) {
+    const float* acc = a.acc + (part0 + x / kQuads) * D + 4 * (x % kQuads);
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const float* p = acc + min(i + j, it.n_parts - 1) * step * D;
+      lo[j] = get_pair(p);
+      hi[j] = get_pair(p + 2);
+    }
+  };
+  if (tid < rows * kQuads) read(tid, 0);  // on its way while the weights are worked out
+  // the pieces' weights, in the memory of the wavefronts' results
+  float* weight = flds;                      // [rows][kMaxParts]
+  float* sums = flds + 16 * NC * kMaxParts;  // [rows][2]
   for (int x = tid; x < rows * 8; x += 256) {  // 8 lanes a row
     const int r = x / 8, j = x % 8;
     float2 st[kMaxParts / 8];
@@ -785,19 +798,11 @@ __global__ __launch_bounds__(256, D * NC <= 128 ? 2 : 1) void k_attn_rows(AttnAr
   }
   __syncthreads();
   for (int x = tid; x < rows * kQuads; x += 256) {
-    const int r = x / kQuads, q = x % kQuads;
-    const float* acc = a.acc + (part0 + r) * D + 4 * q;
+    const int r = x / kQuads;
     f32x4 sum{};
-    constexpr int kBatch = NC == 1 ? 8 : 2;  // pieces read at a time
 #pragma unroll 1
     for (int i = 0; i < it.n_parts; i += kBatch) {
-      float2 lo[kBatch], hi[kBatch];
-#pragma unroll
-      for (int j = 0; j < kBatch; ++j) {
-        const float* p = acc + min(i + j, it.n_parts - 1) * step * D;
-        lo[j] = get_pair(p);
-        hi[j] = get_pair(p + 2);
-      }
+      if (x != tid || i > 0) read(x, i);
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
         if (i + j >= it.n_parts) break;
@@ -808,7 +813,7 @@ __global__ __launch_bounds__(256, D * NC <= 128 ? 2 : 1) void k_attn_rows(AttnAr
         sum[3] = fmaf(f, hi[j].y, sum[3]);
       }
     }
-    put_row(r, q, sum, sums[2 * r], sums[2 * r + 1]);
+    put_row(r, x % kQuads, sum, sums[2 * r], sums[2 * r + 1]);
   }
 }
 
@@ -818,6 +823,7 @@ template <class T>
 __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, uint32_t dim, uint32_t fp8) {
   const uint32_t quads = dim / 4, each = 256 / quads;  // rows of a workgroup
   const uint32_t q = threadIdx.x % quads, chunks = 128 / each;
+  if (a.head->sizes != a.sizes) return;
   const uint32_t total = (uint32_t)a.head->n_split * a.kv_heads * chunks;
   for (uint32_t w = blockIdx.x; w < total; w += gridDim.x) {
     const uint32_t r = w % chunks * each + threadIdx.x / quads, head = w / chunks % a.kv_heads;
@@ -861,9 +867,17 @@ kv_status launch_tile(const AttnArgs& a, uint32_t grid, hipStream_t s) {
 template <class T, int D, bool kFp8, int NC>
 kv_status launch_rows(const AttnArgs& a, uint32_t grid, hipStream_t s) {
   const size_t lds = 4 * 16 * NC * (D + 4 + 2) * sizeof(float);
-  static const hipError_t ready = hipFuncSetAttribute((const void*)k_attn_rows<T, D, kFp8, NC>,
-                                                      hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-  KV_HIP(ready);
+  if (lds > 64 * 1024) {  // has to be allowed, once on each device
+    static std::atomic<uint64_t> allowed{0};
+    int dev = 0;
+    KV_HIP(hipGetDevice(&dev));
+    const uint64_t bit = 1ull << (dev & 63);
+    if (!(allowed.load(std::memory_order_relaxed) & bit)) {
+      KV_HIP(hipFuncSetAttribute((const void*)k_attn_rows<T, D, kFp8, NC>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                 (int)lds));
+      allowed.fetch_or(bit, std::memory_order_relaxed);
+    }
+  }
   hipLaunchKernelGGL((k_attn_rows<T, D, kFp8, NC>), dim3(grid), dim3(256), lds, s, a);
   KV_HIP(hipGetLastError());
   return KV_OK;
@@ -905,6 +919,7 @@ kv_status paged_attention(const kv_paged_batch& b, const WorkLayout& w, const kv
   a.k_scale = c.k_scale, a.v_scale = c.v_scale;
   a.table = b.table;
   const uint8_t* at = (const uint8_t*)b.work;
+  a.sizes = work_sizes(b);
   a.head = (const WorkHeader*)at;
   a.items = (const PieceItem*)(at + w.items);
   a.split = (const SplitTile*)(at + w.split);

@@ -21,6 +21,7 @@ struct PlanArgs {
   kv_paged_batch b;
   uint32_t shift;  // log2 of block_size
   uint32_t group, rows, pieces, max_items, max_parts, max_split;
+  uint64_t sizes;
   WorkHeader* head;
   PieceItem* items;
   SplitTile* split;
@@ -302,6 +303,7 @@ __global__ __launch_bounds__(kNT) void k_paged_plan(PlanArgs a) {
   if (tid == 0) {
     a.head->n_items = (int32_t)min(n_items, a.max_items);
     a.head->n_split = (int32_t)min(n_split, a.max_split);
+    a.head->sizes = a.sizes;
   }
 }
 
@@ -313,6 +315,7 @@ kv_status paged_plan(const kv_paged_batch& b, const WorkLayout& w, hipStream_t s
   a.shift = (uint32_t)__builtin_ctz(b.block_size);
   a.group = w.group, a.rows = w.rows, a.pieces = w.pieces;
   a.max_items = w.max_items, a.max_parts = w.max_parts, a.max_split = w.max_split;
+  a.sizes = work_sizes(b);
   uint8_t* at = (uint8_t*)b.work;
   a.head = (WorkHeader*)at;
   a.items = (PieceItem*)(at + w.items);

@@ -24,6 +24,12 @@ bool rope_is_live(const kv_rope* r) {
   return g_ropes.count(r) != 0;
 }
 
+// The table lies on the device it was made on.
+bool rope_is_elsewhere(const kv_rope* r) {
+  int dev = -1;
+  return hipGetDevice(&dev) != hipSuccess || dev != r->device;
+}
+
 kv_status invalid(const char* who, const char* what) {
   return fail(KV_ERR_INVALID, std::string(who) + ": " + what);
 }
@@ -180,6 +186,7 @@ extern "C" kv_status kv_rope_apply(const kv_rope* r, uint32_t dtype, kv_heads_vi
       return invalid(who, "head_dim must be a multiple of 16 in rot_dim..256");
     if (n_heads > 65536) return invalid(who, "n_heads out of range");
     if (n_tokens == 0 || n_heads == 0) return KV_OK;
+    if (kv::rope_is_elsewhere(r)) return invalid(who, "the rotation is on another device");
     if (!pos || !kv::aligned(pos, 4)) return invalid(who, "pos is NULL or misaligned");
     if (const char* e = kv::check_view(x)) return invalid(who, e);
     if (const char* e = kv::check_view(y)) return invalid(who, e);
@@ -213,6 +220,7 @@ extern "C" kv_status kv_paged_append(const kv_paged_batch* b, const kv_paged_cac
     if (const char* e = kv::check_cache(*c, *b, dtype)) return invalid(who, e);
     if (rope && !kv::rope_is_live(rope)) return invalid(who, "not a live rotation");
     if (rope && rope->table.rot_dim > b->head_dim) return invalid(who, "the rotation is wider than a head");
+    if (rope && kv::rope_is_elsewhere(rope)) return invalid(who, "the rotation is on another device");
     if (const char* e = kv::check_view(k)) return invalid(who, e);
     if (const char* e = kv::check_view(v)) return invalid(who, e);
     if (q.ptr) {

@@ -301,3 +301,20 @@ def test_refusals():
         K.kv_paged_attention(p, cache, q.bfloat16())
     with pytest.raises(K.KvError):
         K.kv_paged_attention(p, cache, q, scale=-1.0)
+
+
+def test_a_work_list_for_other_sizes_is_not_followed():
+    import torch
+    from paper_2603_08739_amd import kvpaged as K
+    i32 = dict(dtype=torch.int32, device="cuda")
+    kc, vc = torch.zeros(4, 2, 16, 64, device="cuda").half(), torch.zeros(4, 2, 64, 16, device="cuda").half()
+    for max_new in (1, None):
+        p = K.Plan(2, 2, 16, 2, 4, 2, 64, max_new=max_new)
+        q, out = torch.ones(2, 4, 64, device="cuda").half(), torch.full((2, 4, 64), 3.0, device="cuda").half()
+        K.kv_paged_plan(p, torch.zeros(2, **i32), torch.ones(2, **i32), torch.zeros(2, 2, **i32))
+        p.batch.window = 7
+        K.kv_paged_attention(p, K.Cache(kc, vc), q, out=out)
+        assert bool((out == 3.0).all())
+        p.batch.window = 0
+        K.kv_paged_attention(p, K.Cache(kc, vc), q, out=out)
+        assert bool((out == 0.0).all())
