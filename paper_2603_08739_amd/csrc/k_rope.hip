@@ -126,6 +126,37 @@ __device__ __forceinline__ void turn_unit(float* a, float* b, const Turns& t) {
   }
 }
 
+// A thread's elements of heads first .. end - 1 of a token.  Four heads are read before
+// the first is written: the compiler may not move reads past writes, as y may be x.
+template <class V, bool kHalf>
+__device__ __forceinline__ void turn_heads(const uint16_t* x, int64_t xh, uint16_t* y, int64_t yh, uint32_t first,
+                                           uint32_t end, int lo, int hi, bool turns, const Turns& t) {
+  constexpr uint32_t kAhead = 4;
+  for (uint32_t h = first; h < end; h += kAhead) {
+    uint4 u[kAhead], w[kAhead];
+#pragma unroll
+    for (uint32_t i = 0; i < kAhead; ++i)
+      if (h + i < end) {
+        u[i] = *(const uint4*)(x + (h + i) * xh + lo);
+        w[i] = *(const uint4*)(x + (h + i) * xh + hi);
+      }
+#pragma unroll
+    for (uint32_t i = 0; i < kAhead; ++i)
+      if (h + i < end) {
+        if (turns) {
+          float f[8], g[8];
+          unpack<V>(u[i], f);
+          unpack<V>(w[i], g);
+          turn_unit<kHalf>(f, g, t);
+          u[i] = pack<V>(f);
+          w[i] = pack<V>(g);
+        }
+        *(uint4*)(y + (h + i) * yh + lo) = u[i];
+        *(uint4*)(y + (h + i) * yh + hi) = w[i];
+      }
+  }
+}
+
 struct ApplyArgs {
   const uint64_t* turn;
   const uint16_t* x;
@@ -155,21 +186,7 @@ __global__ __launch_bounds__(256) void k_rope_apply(ApplyArgs a) {
   const uint32_t end = min(a.n_heads, (group + 1) * a.heads_each);
   const uint16_t* x = a.x + (int64_t)token * a.xt;
   uint16_t* y = a.y + (int64_t)token * a.yt;
-  for (uint32_t h = group * a.heads_each; h < end; ++h) {
-    const uint16_t* p = x + h * a.xh;
-    uint16_t* o = y + h * a.yh;
-    uint4 u = *(const uint4*)(p + lo), w = *(const uint4*)(p + hi);
-    if (turns) {
-      float f[8], g[8];
-      unpack<V>(u, f);
-      unpack<V>(w, g);
-      turn_unit<kHalf>(f, g, t);
-      u = pack<V>(f);
-      w = pack<V>(g);
-    }
-    *(uint4*)(o + lo) = u;
-    *(uint4*)(o + hi) = w;
-  }
+  turn_heads<V, kHalf>(x, a.xh, y, a.yh, group * a.heads_each, end, lo, hi, turns, t);
 }
 
 struct AppendArgs {
@@ -213,19 +230,7 @@ __global__ __launch_bounds__(256) void k_append(AppendArgs a) {
       const uint32_t end = min(a.q_heads, (group + 1) * a.heads_each);
       const uint16_t* x = a.q + (int64_t)token * a.qt;
       uint16_t* y = a.q_out + (int64_t)token * a.ot;
-      for (uint32_t h = group * a.heads_each; h < end; ++h) {
-        uint4 u = *(const uint4*)(x + h * a.qh + lo), w = *(const uint4*)(x + h * a.qh + hi);
-        if (turns) {
-          float f[8], g[8];
-          unpack<V>(u, f);
-          unpack<V>(w, g);
-          turn_unit<kHalf>(f, g, t);
-          u = pack<V>(f);
-          w = pack<V>(g);
-        }
-        *(uint4*)(y + h * a.oh + lo) = u;
-        *(uint4*)(y + h * a.oh + hi) = w;
-      }
+      turn_heads<V, kHalf>(x, a.qh, y, a.oh, group * a.heads_each, end, lo, hi, turns, t);
       return;
     }
     const int64_t slot = a.slot[token];
