@@ -217,7 +217,8 @@ __global__ __launch_bounds__(kNT) void k_paged_plan(PlanArgs a) {
   for (int d = 1; d < 64; d <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, d, 64));
   if (lane_id() == 0 && mine) atomicAdd(&total_units, mine), atomicMax(&most_units, most);
   __syncthreads();
-  const uint32_t longest = max(kMinUnits, (uint32_t)((total_units + a.pieces - 1) / a.pieces));
+  const uint32_t least = a.rows < 128 && total_units * a.b.kv_heads <= 256 ? kMinUnitsFew : kMinUnits;
+  const uint32_t longest = max(least, (uint32_t)((total_units + a.pieces - 1) / a.pieces));
   auto cut_of = [&](const Tile& y) { return min(((uint32_t)y.units + longest - 1) / longest, (uint32_t)kMaxParts); };
   // Long pieces go first, so that the last ones to end are short: the list is ordered
   // by classes of length (within one, in any order: results do not depend on it).

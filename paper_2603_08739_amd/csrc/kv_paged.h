@@ -69,8 +69,11 @@ struct WorkLayout {
 };
 
 // A piece is no shorter than this many units: below it, the joining of partial
-// results costs more than the shorter walk saves.
-constexpr uint32_t kMinUnits = 4;
+// results costs more than the shorter walk saves (16 contexts of 1,000 tokens: 16 us,
+// with 2 units 21).  Only where two units a piece leave compute units idle all the same,
+// a step of few tokens and short contexts, they are the faster ones (one context of
+// 501 tokens: 7.3 us a call, with 4 units 8.3).
+constexpr uint32_t kMinUnits = 4, kMinUnitsFew = 2;
 // A tile is cut into no more pieces than this: one workgroup reads them all.  (One
 // context of 131,072 tokens, 8 key/value heads of 128: 101 us with 32 pieces a head,
 // 105 with 64, 130 with 192.)

@@ -70,6 +70,7 @@ for _name in EXPORTS:
 
 _TYPES = {torch.bfloat16: KV_DT_BF16, torch.float16: KV_DT_F16, torch.float8_e4m3fn: KV_DT_FP8}
 _NO_VIEW = kv_heads_view()
+_raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
 
 def _stream(stream):
@@ -77,7 +78,7 @@ def _stream(stream):
     calls take a few microseconds on the device, and torch.cuda.current_stream()
     would take three more: the handle is asked for without making a Stream."""
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return _raw_stream(_device())
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
@@ -95,12 +96,12 @@ def _view(t, name, tokens, heads, dim, dtype=None):
     s = t.shape
     if len(s) != 3 or s[0] < tokens or s[1] != heads or s[2] != dim:
         raise ValueError(f"{name} has shape {tuple(s)}; the call needs [>={tokens}, {heads}, {dim}]")
-    if dtype is not None and t.dtype != dtype:
+    if dtype is not None and t.dtype is not dtype:
         raise ValueError(f"{name} has dtype {t.dtype}; expected {dtype}")
-    st = t.stride()
-    if st[2] != 1:
+    by_token, by_head, by_element = t.stride()
+    if by_element != 1:
         raise ValueError(f"{name}: a head's elements must be contiguous")
-    return kv_heads_view(t.data_ptr(), st[0], st[1])
+    return kv_heads_view(t.data_ptr(), by_token, by_head)
 
 
 def _array(t, name, dtype, numel):
