@@ -200,7 +200,7 @@ __device__ __forceinline__ float2 get_pair(const float* p) {
 constexpr float kSlack = 8.0f;
 
 template <class T, int D, bool kFp8>
-__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attn_tile(AttnArgs a) {
+__global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 4) void k_attn_tile(AttnArgs a) {
   constexpr int BK = 64, kBytes = kFp8 ? 1 : 2;
   typedef TileLds<D, kBytes> L;
   __shared__ uint4 k_lds0[L::kChunks], k_lds1[L::kChunks], v_lds0[L::kChunks], v_lds1[L::kChunks];
@@ -410,6 +410,10 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attn_tile(AttnArgs a)
         break;
       }
       look = true;
+      // Heads of 64: the keys are read again; kept for this, they would take the
+      // registers of a fourth wavefront on each SIMD (a prompt 344 -> 330 us; heads of 128
+      // gain no wavefront, and lose 1 % by it).
+      if (D == 64) asm volatile("" ::: "memory");
     }
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
