@@ -22,7 +22,7 @@ constexpr uint32_t kClasses = 64;  // of piece lengths: one for each lane of a w
 struct PlanArgs {
   kv_paged_batch b;
   uint32_t shift;  // log2 of block_size
-  uint32_t group, rows, pieces, max_items, max_parts, max_split;
+  uint32_t group, rows, pieces, few_pieces, max_items, max_parts, max_split;
   uint64_t sizes;
   WorkHeader* head;
   PieceItem* items;
@@ -220,7 +220,9 @@ __global__ __launch_bounds__(kNT) void k_paged_plan(PlanArgs a) {
   if (lane_id() == 0 && mine) atomicAdd(&total_units, mine), atomicMax(&most_units, most);
   __syncthreads();
   const uint32_t least = a.rows < 128 && total_units * a.b.kv_heads <= 256 ? kMinUnitsFew : kMinUnits;
-  const uint32_t longest = max(least, (uint32_t)((total_units + a.pieces - 1) / a.pieces));
+  uint32_t longest = (uint32_t)((total_units + a.few_pieces - 1) / a.few_pieces);
+  if (longest >= kLongUnits) longest = (uint32_t)((total_units + a.pieces - 1) / a.pieces);
+  longest = max(longest, least);
   auto cut_of = [&](const Tile& y) { return min(((uint32_t)y.units + longest - 1) / longest, (uint32_t)kMaxParts); };
   // Long pieces go first, so that the last ones to end are short: the list is ordered
   // by classes of length (within one, in any order: results do not depend on it).
@@ -316,7 +318,7 @@ kv_status paged_plan(const kv_paged_batch& b, const WorkLayout& w, hipStream_t s
   PlanArgs a{};
   a.b = b;
   a.shift = (uint32_t)__builtin_ctz(b.block_size);
-  a.group = w.group, a.rows = w.rows, a.pieces = w.pieces;
+  a.group = w.group, a.rows = w.rows, a.pieces = w.pieces, a.few_pieces = w.few_pieces;
   a.max_items = w.max_items, a.max_parts = w.max_parts, a.max_split = w.max_split;
   a.sizes = work_sizes(b);
   uint8_t* at = (uint8_t*)b.work;

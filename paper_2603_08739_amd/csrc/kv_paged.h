@@ -63,7 +63,8 @@ struct WorkLayout {
   uint32_t rows;       // rows of a tile: 16, 32 or 64 (one tile a request) or 128
   uint32_t group;      // G
   uint32_t max_tiles;
-  uint32_t pieces;     // pieces wanted per key/value head
+  uint32_t pieces;     // pieces wanted per key/value head,
+  uint32_t few_pieces; // and where they would otherwise be short
   uint32_t max_items, max_parts, max_split;
   uint64_t items, split, done, acc, ml, bytes;  // offsets from work; bytes in all
 };
@@ -74,6 +75,12 @@ struct WorkLayout {
 // a step of few tokens and short contexts, they are the faster ones (one context of
 // 501 tokens: 7.3 us a call, with 4 units 8.3).
 constexpr uint32_t kMinUnits = 4, kMinUnitsFew = 2;
+// Tiles of 128 rows of heads of 64: 1,024 pieces instead of 512 where those would still be
+// at least this long, as joining twice as many costs 2 to 7 us more (300 tokens over
+// 60,000 cached ones, 24 / 4 heads: 156 us, with 512 pieces 199; 8 chunks of 128 tokens over
+// 8,192: 105 and 111; 4 of 512 over 4,096, pieces of 51 units: 98 and 89; 16 of 100 over
+// 1,000: 42 and 35).
+constexpr uint32_t kLongUnits = 64;
 // A tile is cut into no more pieces than this: one workgroup reads them all.  (One
 // context of 131,072 tokens, 8 key/value heads of 128: 101 us with 32 pieces a head,
 // 105 with 64, 130 with 192.)
@@ -94,7 +101,9 @@ inline WorkLayout work_layout(const kv_paged_batch& b) {
   // times as many 119).  128 rows: 512, what the chip holds of heads of 128, as the pieces' partial
   // results are large (8 chunks of 128 tokens over 8,192 cached ones: 203 us, with 1,024
   // pieces 217; ragged chunks with a window: the same with either).
-  w.pieces = ((w.rows < 128 ? 1024 : 512) + b.kv_heads - 1) / b.kv_heads;
+  // Of heads of 64 the chip holds 1,024; so many where kLongUnits says.
+  w.pieces = ((w.rows < 128 || b.head_dim == 64 ? 1024 : 512) + b.kv_heads - 1) / b.kv_heads;
+  w.few_pieces = w.rows < 128 ? w.pieces : (512 + b.kv_heads - 1) / b.kv_heads;
   w.max_items = w.max_tiles + w.pieces;
   w.max_parts = 2 * w.pieces;
   w.max_split = w.pieces;
