@@ -204,9 +204,11 @@ kv_status kv_paged_append(const kv_paged_batch* b, const kv_paged_cache* c, cons
  * token t sees: its request's positions up to its own, within the window, in
  * blocks that are there.  lse[t][h] = log sum_j exp(scale * q.K[j]).  A token
  * that sees nothing gets zeros and -inf.  Masked keys and values count for
- * nothing whatever they hold.  Products are on the matrix cores with 32-bit
- * sums; softmax statistics are in 32 bits; the weights are rounded to the
- * queries' type for the second product.  Results do not depend on timing.
+ * nothing whatever they hold.  Of what is seen, a score of -inf weighs nothing
+ * (no other: as if nothing was seen), one of +inf or NaN leaves NaN in out and
+ * lse.  Products are on the matrix cores with 32-bit sums; softmax statistics
+ * are in 32 bits; the weights are rounded to the queries' type for the second
+ * product.  Results do not depend on timing.
  *   q, out    views of q_heads heads; out must not overlap q
  *   lse       device float [max_tokens][q_heads] or NULL
  *   scale     > 0 and finite

@@ -43,7 +43,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
 struct BF16 {
-  static constexpr float kWeights = 1.0e12f;  // of 32 keys: far from overflow
+  static constexpr float kLift = 0.0f;
   static constexpr uint32_t kExp = 0x7f80u;  // exponent bits: all set = not finite
   static __device__ __forceinline__ float value(uint16_t u) { return (float)__builtin_bit_cast(__bf16, u); }
   static __device__ __forceinline__ f32x16 mfma32(const uint4& a, const uint4& b, const f32x16& c) {
@@ -66,7 +66,9 @@ struct BF16 {
 };
 
 struct F16 {
-  static constexpr float kWeights = 16384.0f;  // none of them overflows to infinity
+  // Weights are up to 2^6 at the running maximum: their small ones, of 24 bits below
+  // 1 in all, then lose less.
+  static constexpr float kLift = 6.0f;
   static constexpr uint32_t kExp = 0x7c00u;
   static __device__ __forceinline__ float value(uint16_t u) { return (float)__builtin_bit_cast(_Float16, u); }
   static __device__ __forceinline__ f32x16 mfma32(const uint4& a, const uint4& b, const f32x16& c) {
@@ -205,8 +207,11 @@ __device__ __forceinline__ float2 get_pair(const float* p) {
 }
 
 // Rescaling is put off until a maximum rises by more than this (base 2): weights
-// then reach 2^8, which their 16-bit types hold with the same relative rounding.
+// then reach 2^8, in float16 2^14, which their 16-bit types hold with the same relative
+// rounding.
 constexpr float kSlack = 8.0f;
+// Or until the weights of 32 keys sum to more than this: none overflows.
+constexpr float kWeights = 16384.0f;
 
 template <class T, int D, bool kFp8>
 __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 4) void k_attn_tile(AttnArgs a) {
@@ -387,7 +392,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 4) void k_attn_t
         for (int n = 0; n < 2; ++n)
 #pragma unroll
           for (int e = 0; e < 16; e += 2) top = max3(top, s[n][e], s[n][e + 1]);
-        top = max2(top, other_half(top)) * c;
+        top = fmaf(max2(top, other_half(top)), c, -T::kLift);
         if (kLazy || __any(top > m + kSlack)) {
           const float m_new = fmaxf(m, top);
           const float alpha = m_new == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
@@ -414,7 +419,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 4) void k_attn_t
                                     T::pack(s[n][8 * h + 4], s[n][8 * h + 5]), T::pack(s[n][8 * h + 6], s[n][8 * h + 7]));
       }
       const float all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-      if (!kLazy || look || !__any(!(all <= T::kWeights))) {
+      if (!kLazy || look || !__any(!(all <= kWeights))) {
         l += all;
         break;
       }
@@ -645,7 +650,7 @@ __global__ __launch_bounds__(256, D * NC <= 128 ? 2 : 1) void k_attn_rows(AttnAr
         top = max3(top, s[n][b][2], s[n][b][3]);
       }
       top = max2(top, __shfl_xor(top, 16, 64));
-      top = max2(top, other_half(top)) * c;
+      top = fmaf(max2(top, other_half(top)), c, -T::kLift);
       if (__any(top > m[n] + kSlack)) {
         const float m_new = fmaxf(m[n], top);
         const float alpha = m_new == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m[n] - m_new);

@@ -318,3 +318,74 @@ def test_a_work_list_for_other_sizes_is_not_followed():
         p.batch.window = 0
         K.kv_paged_attention(p, K.Cache(kc, vc), q, out=out)
         assert bool((out == 0.0).all())
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("new, kept", [(1, "f16"), (1, "fp8"), (150, "f16"), (150, "fp8")])
+def test_many_small_weights(dim, new, kept):
+    """One key outweighs the others, and its value is zero: what remains is a sum of
+    weights near 2^-17, whose rounding has to be relative (as multiples of float16's
+    smallest number they would be off by 2^-8; the scores are chosen for that)."""
+    score = 11.8515625 if kept == "f16" else 11.0    # exact in the cache's type; of 8 bits, times 32 and the head's scale
+
+    def edit(kc, vc, table):
+        kc.zero_()
+        vc.fill_(1.0)
+        first = int(table[0, 0])
+        kc[first, :, 0, 0] = score
+        vc[first, :, :, 0] = 0.0
+
+    def edit_q(q):
+        q.zero_()
+        q[..., 0] = 1.0
+    out, _ = case([700], [new], 64, (8, 2), dim, "f16", kept, max_new=1 if new == 1 else None, edit=edit, edit_q=edit_q, scale=1.0 if kept == "f16" else 32.0)
+    assert bool((out > 0).all())
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("new", [1, 150])
+def test_large_values_while_scores_rise(dim, new):
+    """Scores rise by 2^30 in weight from one run of keys to the next, over values of
+    10^30: nothing on the way to their average passes the 32-bit range."""
+    def edit(kc, vc, table):
+        kc.zero_()
+        vc.fill_(1.0e30)
+        for col in range(table.shape[1]):
+            kc[int(table[0, col]), :, :, 0] = 20.75 * col
+
+    def edit_q(q):
+        q.zero_()
+        q[..., 0] = 1.0
+    out, _ = case([700], [new], 64, (8, 2), dim, "bf16", "bf16", max_new=1 if new == 1 else None, edit=edit, edit_q=edit_q, scale=1.0)
+    assert bool((out > 9.0e29).all())
+
+
+@pytest.mark.parametrize("new", [1, 150])
+def test_infinite_scores(new):
+    """A score of -inf weighs nothing, where there is no other the query sees nothing;
+    one of +inf leaves NaN, in the log-sum-exp as well."""
+    import torch
+    from oracle import paged as O
+    from paper_2603_08739_amd import kvpaged as K
+    i32 = dict(dtype=torch.int32, device="cuda")
+    gen = torch.Generator().manual_seed(4)
+    kc, vc = torch.randn(8, 1, 64, 64, generator=gen).bfloat16().cuda(), torch.randn(8, 1, 64, 64, generator=gen).bfloat16().cuda()
+    q = torch.randn(new, 3, 64, generator=gen).bfloat16().cuda()
+    table = torch.arange(8, **i32).view(1, 8)
+    q[:, 0, 5], q[:, 1, 5], q[:, 2, 5] = -1.0, 1.0, -1.0
+    q[:, 2, 6] = -1.0
+    kc[3, 0, 7, 5] = float("inf")                     # heads 0, 2: -inf; head 1: +inf
+    kc[:, 0, :, 6] = torch.where(torch.isinf(kc[:, 0, :, 5]), 0.0, 1.0).to(kc.dtype)
+    p = K.Plan(1, new, 64, 8, 3, 1, 64, max_new=1 if new == 1 else None)
+    K.kv_paged_plan(p, torch.full((1,), 300, **i32), torch.full((1,), new, **i32), table)
+    lse = torch.empty(new, 3, device="cuda")
+    out = K.kv_paged_attention(p, K.Cache(kc, vc), q, lse=lse)
+    assert bool(torch.isnan(out[:, 1]).all()) and bool(torch.isnan(lse[:, 1]).all())
+    want, want_lse, spread, _ = O.attention(q, kc, vc, table.tolist(), p.q_start.tolist(), [300], 64, 8, 64 ** -0.5, 0)
+    for h in (0, 2):   # scores of less than 2^7: 64 products are off by less than 2^-10
+        err = (out[:, h].double() - want[:, h]).abs()
+        assert bool((err <= (2.0 ** -8 + 2.0 ** -9) * spread[:, h] + 2.0 ** -8 * want[:, h].abs()).all())
+        assert bool(((lse[:, h].double() - want_lse[:, h]).abs() <= 2.0 ** -10).all())
+    kc[:, :, :, 5] = float("inf")                     # heads 0 and 2: nothing but -inf
+    K.kv_paged_attention(p, K.Cache(kc, vc), q, out=out, lse=lse)
+    assert bool((out[:, 0] == 0).all()) and bool((out[:, 2] == 0).all()) and bool((lse[:, 0] == -math.inf).all())
