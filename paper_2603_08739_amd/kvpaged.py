@@ -237,6 +237,8 @@ def kv_paged_append(plan: Plan, cache: Cache, k, v, q=None, q_out=None, rope: Ro
     n, dim = b.max_tokens, b.head_dim
     if (q is None) != (q_out is None):
         raise ValueError("q and q_out go together")
+    if rope is not None and rope.handle is None:  # NULL would mean that nothing turns
+        raise ValueError("the rotation has been freed")
     vk, vv = _view(k, "k", n, b.kv_heads, dim), _view(v, "v", n, b.kv_heads, dim, k.dtype)
     vq = _NO_VIEW if q is None else _view(q, "q", n, b.q_heads, dim, k.dtype)
     vo = _NO_VIEW if q is None else _view(q_out, "q_out", n, b.q_heads, dim, k.dtype)
