@@ -209,7 +209,8 @@ kv_status kv_paged_append(const kv_paged_batch* b, const kv_paged_cache* c, cons
  * lse.  Products are on the matrix cores with 32-bit sums; softmax statistics
  * are in 32 bits; the weights are rounded to the queries' type for the second
  * product.  Results do not depend on timing.
- *   q, out    views of q_heads heads; out must not overlap q
+ *   q, out    views of q_heads heads; out must not overlap q (the
+ *             same pointer is KV_ERR_INVALID)
  *   lse       device float [max_tokens][q_heads] or NULL
  *   scale     > 0 and finite
  * Rows past the step's last token are left alone.  The batch must have been

@@ -105,18 +105,18 @@ using kv::invalid;
 
 extern "C" kv_status kv_rope_create(const kv_rope_desc* d, kv_rope** out) {
   const char* who = "kv_rope_create";
-  if (!out) return invalid(who, "out is NULL");
-  *out = nullptr;
-  if (!d) return invalid(who, "desc is NULL");
-  if (d->rot_dim < 16 || d->rot_dim > 256 || d->rot_dim % 16) return invalid(who, "rot_dim must be a multiple of 16 in 16..256");
-  if (d->layout > KV_ROPE_INTERLEAVED) return invalid(who, "unknown layout");
-  if (d->scaling > KV_ROPE_BY_PARTS) return invalid(who, "unknown scaling");
-  if (!(d->base > 1) || !std::isfinite(d->base)) return invalid(who, "base must be > 1 and finite");
-  if (!std::isfinite(d->magnitude) || d->magnitude == 0) return invalid(who, "magnitude must be finite and not 0");
-  if (d->scaling != KV_ROPE_PLAIN && (!(d->factor >= 1) || !std::isfinite(d->factor))) return invalid(who, "factor must be >= 1 and finite");
-  if (d->scaling == KV_ROPE_BY_PARTS && (!d->original_len || !(d->slow >= 0) || !(d->fast > d->slow) || !std::isfinite(d->fast)))
-    return invalid(who, "BY_PARTS needs original_len > 0 and fast > slow >= 0");
   return guarded(who, [&]() -> kv_status {
+    if (!out) return invalid(who, "out is NULL");
+    *out = nullptr;
+    if (!d) return invalid(who, "desc is NULL");
+    if (d->rot_dim < 16 || d->rot_dim > 256 || d->rot_dim % 16) return invalid(who, "rot_dim must be a multiple of 16 in 16..256");
+    if (d->layout > KV_ROPE_INTERLEAVED) return invalid(who, "unknown layout");
+    if (d->scaling > KV_ROPE_BY_PARTS) return invalid(who, "unknown scaling");
+    if (!(d->base > 1) || !std::isfinite(d->base)) return invalid(who, "base must be > 1 and finite");
+    if (!std::isfinite(d->magnitude) || d->magnitude == 0) return invalid(who, "magnitude must be finite and not 0");
+    if (d->scaling != KV_ROPE_PLAIN && (!(d->factor >= 1) || !std::isfinite(d->factor))) return invalid(who, "factor must be >= 1 and finite");
+    if (d->scaling == KV_ROPE_BY_PARTS && (!d->original_len || !(d->slow >= 0) || !(d->fast > d->slow) || !std::isfinite(d->fast)))
+      return invalid(who, "BY_PARTS needs original_len > 0 and fast > slow >= 0");
     const double kTurn = 6.283185307179586476925;
     std::vector<uint64_t> turn(d->rot_dim / 2);
     for (uint32_t i = 0; i < turn.size(); ++i) {
@@ -196,10 +196,12 @@ extern "C" kv_status kv_rope_apply(const kv_rope* r, uint32_t dtype, kv_heads_vi
 
 extern "C" kv_status kv_paged_work_bytes(const kv_paged_batch* b, uint64_t* bytes) {
   const char* who = "kv_paged_work_bytes";
-  if (!b || !bytes) return invalid(who, "NULL argument");
-  if (const char* e = kv::check_sizes(*b)) return invalid(who, e);
-  *bytes = kv::work_layout(*b).bytes;
-  return KV_OK;
+  return guarded(who, [&]() -> kv_status {
+    if (!b || !bytes) return invalid(who, "NULL argument");
+    if (const char* e = kv::check_sizes(*b)) return invalid(who, e);
+    *bytes = kv::work_layout(*b).bytes;
+    return KV_OK;
+  });
 }
 
 extern "C" kv_status kv_paged_plan(const kv_paged_batch* b, void* stream) {
@@ -242,6 +244,8 @@ extern "C" kv_status kv_paged_attention(const kv_paged_batch* b, const kv_paged_
     if (const char* e = kv::check_view(out)) return invalid(who, e);
     if (!(scale > 0) || !std::isfinite(scale)) return invalid(who, "scale must be > 0 and finite");
     if (!kv::aligned(lse, 4)) return invalid(who, "lse is misaligned");
+    // workgroups read queries after others have written their outputs
+    if (out.ptr == q.ptr) return invalid(who, "out must not be q");
     return kv::paged_attention(*b, kv::work_layout(*b), *c, dtype, q, out, lse, scale, (hipStream_t)stream);
   });
 }

@@ -135,6 +135,12 @@ def test_heads_and_scales_are_refused():
     refused(K, append(rope=0x1000), "rotation")
 
 
+def test_attention_in_place_is_refused():
+    from paper_2603_08739_amd import kvpaged as K
+    b, c, w = batch(K), cache(K), view(K)
+    refused(K, K.LIB.kv_paged_attention(ctypes.byref(b), ctypes.byref(c), 0, w, w, None, 1.0, None), "must not be q")
+
+
 @pytest.mark.parametrize("more, word", [
     (dict(rot_dim=0), "rot_dim"), (dict(rot_dim=24), "rot_dim"), (dict(rot_dim=272), "rot_dim"), (dict(layout=2), "layout"),
     (dict(scaling=3), "scaling"), (dict(base=1.0), "base"), (dict(base=float("inf")), "base"), (dict(magnitude=0.0), "magnitude"),
