@@ -164,8 +164,8 @@ __device__ __forceinline__ float element(const uint8_t* p) {
 // lanes in order, so the lane picks the chunk of memory that belongs there).
 //
 // One prompt of 8,111 tokens after 256 cached ones, 32 query and 8 key/value heads of
-// 128, bf16: 573 GFLOP over the keys that queries see in 557 to 602 us (cards
-// differ), 1.0 PFLOP/s where a large matrix product does 1.3 to 1.4.  The matrix
+// 128, bf16: 573 GFLOP over the keys that queries see in 557 to 619 us (cards
+// differ), 0.93 to 1.03 PFLOP/s where a large matrix product does 1.3 to 1.4.  The matrix
 // cores are busy half of the time: the exponentials, conversions and masks take
 // vector instructions, of which two wavefronts on a SIMD hide a part only.  Heads of
 // 64: 870 TFLOP/s, heads of 256: 700.  What was tried beside it and was no faster: the
