@@ -14,9 +14,10 @@
 // sines and cosines once and walks over heads with them.  8,191 tokens of 40 heads
 // of 128 (168 MB read and written) take 36.5 us, 4.6 TB/s, where a large copy does
 // 4.8; 64 tokens of 32 heads 6.0 us a call, which is the host's time, and 2.7 in a
-// graph of 100 calls.  The writes of a chunk's queries, keys and values (212 MB) take 51 us, 4.1 TB/s: V^T is written in runs of
-// a block's tokens, 128 bytes where blocks have 64; into an 8-bit cache of
-// blocks of 16 tokens 42 MB take 11.7 us.
+// graph of 100 calls (caches warm).  The writes of a chunk's queries, keys and
+// values (212 MB) take 51 us, 4.1 TB/s: V^T is written in runs of a block's tokens,
+// 128 bytes where blocks have 64; into an 8-bit cache of blocks of 16 tokens 42 MB
+// take 11.7 us.
 #include "kv_device.h"
 #include "kv_paged.h"
 
