@@ -173,7 +173,9 @@ class Plan:
         b.slot, b.pos, b.result = self.slot.data_ptr(), self.pos.data_ptr(), self.result.data_ptr()
         b.work, b.work_bytes = self.work.data_ptr(), size.value
         self.ref = ctypes.byref(b)
-        self.inputs = None  # kept alive: the later calls of the step read the table
+        # the planned step's tensors, kept alive as the later calls of the step read the
+        # table, and what the batch says of them
+        self.inputs, self.step = None, (None, None, None, 0, None)
 
 
 def kv_paged_plan(plan: Plan, ctx_len, new_len, table, free_list=None, stream=None):
@@ -183,14 +185,20 @@ def kv_paged_plan(plan: Plan, ctx_len, new_len, table, free_list=None, stream=No
     if table.dim() != 2 or table.shape[1] != b.max_blocks:
         raise ValueError(f"table has shape {tuple(table.shape)}; the plan's rows have {b.max_blocks} blocks")
     i32 = torch.int32
-    b.ctx_len = _array(ctx_len, "ctx_len", i32, b.n_req)
-    b.new_len = _array(new_len, "new_len", i32, b.n_req)
-    b.table = _array(table, "table", i32, b.n_req * b.max_blocks)
-    b.n_free = 0 if free_list is None else free_list.numel()
-    # an empty tensor has no address, and NULL would mean that table names every block
-    b.free_list = None if free_list is None else _array(free_list, "free_list", i32, 0) or b.result
-    plan.inputs = (ctx_len, new_len, table, free_list)
-    _check(LIB.kv_paged_plan(plan.ref, _stream(stream)))
+    # all of it is checked before the batch points at any of it: after a refusal the
+    # batch is that of the step planned before, whose tensors are kept
+    step = (_array(ctx_len, "ctx_len", i32, b.n_req), _array(new_len, "new_len", i32, b.n_req),
+            _array(table, "table", i32, b.n_req * b.max_blocks), 0 if free_list is None else free_list.numel(),
+            # an empty tensor has no address, and NULL would mean that table names every block
+            None if free_list is None else _array(free_list, "free_list", i32, 0) or b.result)
+    stream = _stream(stream)
+    b.ctx_len, b.new_len, b.table, b.n_free, b.free_list = step
+    try:
+        _check(LIB.kv_paged_plan(plan.ref, stream))
+    except KvError:
+        b.ctx_len, b.new_len, b.table, b.n_free, b.free_list = plan.step
+        raise
+    plan.inputs, plan.step = (ctx_len, new_len, table, free_list), step
 
 
 class Cache:

@@ -1,0 +1,98 @@
+"""The paged-cache binding without a device: what a refused call leaves behind, what it
+checks and where it allocates.  Tensors lie on the host and say that they are on a GPU;
+the library is a recorder that refuses when told to."""
+import pytest
+import torch
+
+
+class OnGpu(torch.Tensor):
+    """A host tensor that passes for one on GPU `dev`."""
+    dev = 0
+    is_cuda = property(lambda self: True)
+
+    def get_device(self):
+        return self.dev
+
+
+def on_gpu(t, dev=0):
+    x = torch.Tensor._make_subclass(OnGpu, t)
+    x.dev = dev
+    return x
+
+
+class Recorder:
+    """Stands in for the library: keeps the calls, answers with `status`."""
+
+    def __init__(self, K):
+        self.calls, self.status, self.real = [], K.KV_OK, K.LIB
+
+    def __getattr__(self, name):
+        if name in ("kv_paged_work_bytes", "kv_last_error"):
+            return getattr(self.real, name)
+
+        def call(*args):
+            self.calls.append((name, args))
+            return self.status
+        return call
+
+
+@pytest.fixture
+def binding(monkeypatch):
+    from paper_2603_08739_amd import kvpaged as K
+    lib = Recorder(K)
+    monkeypatch.setattr(K, "LIB", lib)
+    monkeypatch.setattr(K, "_device", lambda: 0)
+    monkeypatch.setattr(K, "_raw_stream", lambda dev: 70 + dev)
+    return K, lib
+
+
+def step(n_free=3):
+    i32 = dict(dtype=torch.int32)
+    return [on_gpu(torch.zeros(*s, **i32)) for s in ((2,), (2,), (2, 4), (n_free,))]
+
+
+def plan_for(K):
+    p = K.Plan(2, 8, 16, 4, 4, 2, 64, device="cpu")
+    for name in ("q_start", "kv_len", "slot", "pos", "result", "work"):
+        setattr(p, name, on_gpu(getattr(p, name)))
+    return p
+
+
+def aim(p):
+    b = p.batch
+    return b.ctx_len, b.new_len, b.table, b.n_free, b.free_list
+
+
+@pytest.mark.parametrize("at, bad", [
+    (0, lambda t: t.long()), (1, lambda t: t[:1]), (2, lambda t: t[:1]), (2, lambda t: t[:, :3].contiguous()), (2, lambda t: t.T),
+    (3, lambda t: t.long()), (3, lambda t: torch.zeros(6, dtype=torch.int32)[::2])])
+def test_a_refused_plan_leaves_the_earlier_one(binding, at, bad):
+    """The batch goes on pointing at the step that was planned, whose tensors are kept
+    alive; never at a refused one's, which nobody keeps."""
+    K, lib = binding
+    p, first = plan_for(K), step()
+    K.kv_paged_plan(p, *first)
+    before = aim(p)
+    assert before[:3] == tuple(t.data_ptr() for t in first[:3]) and before[3:] == (3, first[3].data_ptr())
+    second = step(5)
+    second[at] = on_gpu(bad(second[at]))
+    with pytest.raises(ValueError):
+        K.kv_paged_plan(p, *second)
+    assert aim(p) == before and len(lib.calls) == 1
+    assert all(a is b for a, b in zip(p.inputs, first))
+
+
+def test_a_plan_that_the_library_refuses_leaves_the_earlier_one(binding):
+    K, lib = binding
+    p, first = plan_for(K), step()
+    lib.status = K.KV_ERR_INVALID
+    with pytest.raises(K.KvError):
+        K.kv_paged_plan(p, *first)
+    assert aim(p) == (None, None, None, 0, None) and p.inputs is None
+    lib.status = K.KV_OK
+    K.kv_paged_plan(p, *first)
+    before = aim(p)
+    lib.status = K.KV_ERR_INVALID
+    with pytest.raises(K.KvError):
+        K.kv_paged_plan(p, *step(5))
+    assert aim(p) == before and all(a is b for a, b in zip(p.inputs, first))
