@@ -8,6 +8,13 @@ serving step is
     kv_paged_plan(plan, ctx_len, new_len, table, free_list)          # once a step
     kv_paged_append(plan, cache, k, v, q=q, q_out=q, rope=rope)      # every layer
     kv_paged_attention(plan, cache, q, out=out)
+
+Calls go to the current stream, or to `stream`: a torch.cuda.Stream or a stream's handle.
+With a stream that is not the current one the rules are torch's: the inputs have to be
+ready on it, their memory must not be given away before it is done with them, and an
+output that the call makes (out=None) belongs to it: the current stream waits for it
+before a use, and such a use is recorded (Tensor.record_stream) if the output may be
+dropped before it ends.
 """
 from __future__ import annotations
 
@@ -82,6 +89,18 @@ def _stream(stream):
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
+def _output(like, shape, stream):
+    """An output of `like`'s type, made under the stream that will write it: the memory
+    is then none that another stream may still be working on, and is not given to
+    another stream while this one writes."""
+    if stream is None or _stream(stream) == _stream(None):
+        return torch.empty(shape, dtype=like.dtype, device=like.device)
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device=like.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=like.dtype, device=like.device)
+
+
 def _dtype(t, name):
     d = _TYPES.get(t.dtype)
     if d is None or d == KV_DT_FP8:
@@ -141,7 +160,7 @@ def kv_rope_apply(rope: Rope, x, pos, out=None, backward=False, stream=None):
     pos: int32 [tokens]; out: like x (may be x), made when None.  Returns out."""
     n, heads, dim = x.shape
     if out is None:
-        out = torch.empty((n, heads, dim), dtype=x.dtype, device=x.device)
+        out = _output(x, (n, heads, dim), stream)
     vx, vy = _view(x, "x", n, heads, dim), _view(out, "out", n, heads, dim, x.dtype)
     _check(LIB.kv_rope_apply(rope.handle, _dtype(x, "x"), vx, vy,
                              _array(pos, "pos", torch.int32, n), n, heads, dim,
@@ -260,7 +279,7 @@ def kv_paged_attention(plan: Plan, cache: Cache, q, out=None, lse=None, scale=No
     b = _fits(plan, cache)
     n, heads, dim = b.max_tokens, b.q_heads, b.head_dim
     if out is None:
-        out = torch.empty((n, heads, dim), dtype=q.dtype, device=q.device)
+        out = _output(q, (n, heads, dim), stream)
     vq, vo = _view(q, "q", n, heads, dim), _view(out, "out", n, heads, dim, q.dtype)
     pl = None if lse is None else _array(lse, "lse", torch.float32, n * heads)
     _check(LIB.kv_paged_attention(plan.ref, cache.ref, _dtype(q, "q"), vq, vo, pl,

@@ -96,3 +96,56 @@ def test_a_plan_that_the_library_refuses_leaves_the_earlier_one(binding):
     with pytest.raises(K.KvError):
         K.kv_paged_plan(p, *step(5))
     assert aim(p) == before and all(a is b for a, b in zip(p.inputs, first))
+
+
+class Side:
+    cuda_stream, device_index = 1234, 0
+
+
+@pytest.fixture
+def places(monkeypatch):
+    """The handles of the streams that tensors are made under (None: the current one)."""
+    made, under = [], []
+    real = torch.empty
+
+    class Under:
+        def __init__(self, s):
+            self.s = s
+
+        def __enter__(self):
+            under.append(self.s.cuda_stream)
+
+        def __exit__(self, *_):
+            under.pop()
+
+    class External:
+        def __init__(self, handle, device=None):
+            self.cuda_stream, self.device_index = handle, 0
+
+    def empty(*a, device=None, **kw):
+        made.append(under[-1] if under else None)
+        return on_gpu(real(*a, **kw))
+    monkeypatch.setattr(torch.cuda, "stream", Under)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", External)
+    monkeypatch.setattr(torch, "empty", empty)
+    return made
+
+
+@pytest.mark.parametrize("stream, where, handle", [(None, None, 70), (70, None, 70), (Side, 1234, 1234), (1234, 1234, 1234), (0, 0, 0)])
+def test_outputs_are_made_under_the_stream_that_writes_them(binding, places, stream, where, handle):
+    """Memory that the current stream still works on is not given to another stream's
+    call, nor back to the current stream while the other one writes."""
+    K, lib = binding
+    p = plan_for(K)
+    K.kv_paged_plan(p, *step())
+    f16 = dict(dtype=torch.float16)
+    x = on_gpu(torch.zeros(8, 4, 64, **f16))
+    cache = K.Cache(on_gpu(torch.zeros(3, 2, 16, 64, **f16)), on_gpu(torch.zeros(3, 2, 64, 16, **f16)))
+    rope = K.Rope.__new__(K.Rope)
+    rope.handle = 5
+    places.clear()
+    out = K.kv_paged_attention(p, cache, x, stream=stream)
+    assert out.shape == x.shape and out.dtype == x.dtype and places == [where] and lib.calls[-1][1][-1] == handle
+    out = K.kv_rope_apply(rope, x, on_gpu(torch.zeros(8, dtype=torch.int32)), stream=stream)
+    assert out.shape == x.shape and out.dtype == x.dtype and places == [where] * 2 and lib.calls[-1][1][-1] == handle
+    rope.handle = None
