@@ -30,10 +30,8 @@ def test_outputs_do_not_take_memory_of_the_current_stream(as_handle):
         del freed
         out = call(stream=stream)
         assert out.data_ptr() not in addresses
-        back = [torch.empty_like(x) for _ in range(4)]
-        assert {t.data_ptr() for t in back} <= addresses
         torch.cuda.current_stream().wait_stream(side)
         assert torch.equal(out, ref)
-        again = call(out=back[0])
+        again = call(out=torch.empty_like(x))
         assert torch.equal(again, ref)
     rope.free()
