@@ -9,12 +9,12 @@ serving step is
     kv_paged_append(plan, cache, k, v, q=q, q_out=q, rope=rope)      # every layer
     kv_paged_attention(plan, cache, q, out=out)
 
-Calls go to the current stream, or to `stream`: a torch.cuda.Stream or a stream's handle.
-With a stream that is not the current one the rules are torch's: the inputs have to be
-ready on it, their memory must not be given away before it is done with them, and an
-output that the call makes (out=None) belongs to it: the current stream waits for it
-before a use, and such a use is recorded (Tensor.record_stream) if the output may be
-dropped before it ends.
+Tensors, plan, cache and rotation are on the current device.  Calls go to the current
+stream, or to `stream`: a torch.cuda.Stream or a stream's handle.  With a stream that
+is not the current one the rules are torch's: the inputs have to be ready on it, their
+memory must not be given away before it is done with them, and an output that the call
+makes (out=None) belongs to it: the current stream waits for it before a use, and such
+a use is recorded (Tensor.record_stream) if the output may be dropped before it ends.
 """
 from __future__ import annotations
 
@@ -80,20 +80,24 @@ _NO_VIEW = kv_heads_view()
 _raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
 
-def _stream(stream):
-    """The stream's handle; None is the current stream of the current device.  These
+def _stream(stream, dev):
+    """The stream's handle; None is the current stream of the current device `dev`.  These
     calls take a few microseconds on the device, and torch.cuda.current_stream()
     would take three more: the handle is asked for without making a Stream."""
     if stream is None:
-        return _raw_stream(_device())
-    return stream if isinstance(stream, int) else stream.cuda_stream
+        return _raw_stream(dev)
+    if isinstance(stream, int):
+        return stream
+    if getattr(stream, "device_index", dev) != dev:
+        raise ValueError(f"the stream is on device {stream.device_index}; the current device is {dev}")
+    return stream.cuda_stream
 
 
-def _output(like, shape, stream):
+def _output(like, shape, stream, dev):
     """An output of `like`'s type, made under the stream that will write it: the memory
     is then none that another stream may still be working on, and is not given to
     another stream while this one writes."""
-    if stream is None or _stream(stream) == _stream(None):
+    if stream is None or _stream(stream, dev) == _raw_stream(dev):
         return torch.empty(shape, dtype=like.dtype, device=like.device)
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream, device=like.device)
@@ -108,10 +112,10 @@ def _dtype(t, name):
     return d
 
 
-def _view(t, name, tokens, heads, dim, dtype=None):
-    """[tokens, heads, dim] with contiguous elements, at least `tokens` rows."""
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a CUDA tensor")
+def _view(t, name, dev, tokens, heads, dim, dtype=None):
+    """[tokens, heads, dim] on device `dev` with contiguous elements, at least `tokens` rows."""
+    if t.get_device() != dev:
+        raise ValueError(f"{name} must be a CUDA tensor of the current device")
     s = t.shape
     if len(s) != 3 or s[0] < tokens or s[1] != heads or s[2] != dim:
         raise ValueError(f"{name} has shape {tuple(s)}; the call needs [>={tokens}, {heads}, {dim}]")
@@ -123,10 +127,10 @@ def _view(t, name, tokens, heads, dim, dtype=None):
     return kv_heads_view(t.data_ptr(), by_token, by_head)
 
 
-def _array(t, name, dtype, numel):
-    """A contiguous CUDA tensor of this dtype with at least `numel` elements."""
-    if not t.is_cuda or t.dtype != dtype or not t.is_contiguous() or t.numel() < numel:
-        raise ValueError(f"{name} must be a contiguous CUDA {dtype} tensor of at least {numel} elements")
+def _array(t, name, dev, dtype, numel):
+    """A contiguous tensor of this dtype on device `dev` with at least `numel` elements."""
+    if t.get_device() != dev or t.dtype != dtype or not t.is_contiguous() or t.numel() < numel:
+        raise ValueError(f"{name} must be a contiguous CUDA {dtype} tensor of the current device, of at least {numel} elements")
     return t.data_ptr()
 
 
@@ -158,13 +162,15 @@ class Rope:
 def kv_rope_apply(rope: Rope, x, pos, out=None, backward=False, stream=None):
     """x: [tokens, heads, dim] bfloat16 / float16 at any token and head stride;
     pos: int32 [tokens]; out: like x (may be x), made when None.  Returns out."""
+    dev = _device()
     n, heads, dim = x.shape
+    vx = _view(x, "x", dev, n, heads, dim)
     if out is None:
-        out = _output(x, (n, heads, dim), stream)
-    vx, vy = _view(x, "x", n, heads, dim), _view(out, "out", n, heads, dim, x.dtype)
+        out = _output(x, (n, heads, dim), stream, dev)
+    vy = _view(out, "out", dev, n, heads, dim, x.dtype)
     _check(LIB.kv_rope_apply(rope.handle, _dtype(x, "x"), vx, vy,
-                             _array(pos, "pos", torch.int32, n), n, heads, dim,
-                             1 if backward else 0, _stream(stream)))
+                             _array(pos, "pos", dev, torch.int32, n), n, heads, dim,
+                             1 if backward else 0, _stream(stream, dev)))
     return out
 
 
@@ -183,6 +189,7 @@ class Plan:
         size = _u64()
         _check(LIB.kv_paged_work_bytes(ctypes.byref(b), ctypes.byref(size)))
         self.q_start = torch.empty(b.n_req + 1, dtype=torch.int32, device=device)
+        self.dev = self.q_start.get_device()
         self.kv_len = torch.empty(b.n_req, dtype=torch.int32, device=device)
         self.slot = torch.empty(b.max_tokens, dtype=torch.int64, device=device)
         self.pos = torch.empty(b.max_tokens, dtype=torch.int32, device=device)
@@ -200,17 +207,19 @@ class Plan:
 def kv_paged_plan(plan: Plan, ctx_len, new_len, table, free_list=None, stream=None):
     """ctx_len, new_len: int32 [n_req]; table: int32 [n_req, max_blocks], written
     where a request takes new blocks from free_list (int32), read otherwise."""
-    b = plan.batch
+    b, dev = plan.batch, _device()
+    if plan.dev != dev:
+        raise ValueError(f"the plan is on device {plan.dev}; the current device is {dev}")
     if table.dim() != 2 or table.shape[1] != b.max_blocks:
         raise ValueError(f"table has shape {tuple(table.shape)}; the plan's rows have {b.max_blocks} blocks")
     i32 = torch.int32
     # all of it is checked before the batch points at any of it: after a refusal the
     # batch is that of the step planned before, whose tensors are kept
-    step = (_array(ctx_len, "ctx_len", i32, b.n_req), _array(new_len, "new_len", i32, b.n_req),
-            _array(table, "table", i32, b.n_req * b.max_blocks), 0 if free_list is None else free_list.numel(),
+    step = (_array(ctx_len, "ctx_len", dev, i32, b.n_req), _array(new_len, "new_len", dev, i32, b.n_req),
+            _array(table, "table", dev, i32, b.n_req * b.max_blocks), 0 if free_list is None else free_list.numel(),
             # an empty tensor has no address, and NULL would mean that table names every block
-            None if free_list is None else _array(free_list, "free_list", i32, 0) or b.result)
-    stream = _stream(stream)
+            None if free_list is None else _array(free_list, "free_list", dev, i32, 0) or b.result)
+    stream = _stream(stream, dev)
     b.ctx_len, b.new_len, b.table, b.n_free, b.free_list = step
     try:
         _check(LIB.kv_paged_plan(plan.ref, stream))
@@ -228,6 +237,9 @@ class Cache:
     def __init__(self, k, v, k_scale=None, v_scale=None):
         if k.dim() != 4 or v.dim() != 4 or not k.is_cuda or not v.is_cuda:
             raise ValueError("k and v must be CUDA tensors of four dimensions")
+        dev = self.dev = k.get_device()
+        if v.get_device() != dev:
+            raise ValueError("k and v must be on one device")
         n, heads, block, dim = k.shape
         if tuple(v.shape) != (n, heads, dim, block) or v.dtype != k.dtype or k.dtype not in _TYPES:
             raise ValueError(f"v has shape {tuple(v.shape)} and dtype {v.dtype}, k {tuple(k.shape)} and {k.dtype}")
@@ -241,13 +253,15 @@ class Cache:
         c.k_block_stride = k.stride(0) if n > 1 else one
         c.v_block_stride = v.stride(0) if n > 1 else one
         c.n_blocks, c.dtype = n, _TYPES[k.dtype]
-        c.k_scale = None if k_scale is None else _array(k_scale, "k_scale", torch.float32, heads)
-        c.v_scale = None if v_scale is None else _array(v_scale, "v_scale", torch.float32, heads)
+        c.k_scale = None if k_scale is None else _array(k_scale, "k_scale", dev, torch.float32, heads)
+        c.v_scale = None if v_scale is None else _array(v_scale, "v_scale", dev, torch.float32, heads)
         self.ref = ctypes.byref(c)
 
 
-def _fits(plan, cache):
+def _fits(plan, cache, dev):
     b = plan.batch
+    if plan.dev != dev or cache.dev != dev:
+        raise ValueError(f"the plan is on device {plan.dev}, the cache on {cache.dev}; the current device is {dev}")
     if cache.shape != (b.kv_heads, b.block_size, b.head_dim):
         raise ValueError(f"the cache's heads, block and head size are {cache.shape}; "
                          f"the plan's {(b.kv_heads, b.block_size, b.head_dim)}")
@@ -260,28 +274,31 @@ def kv_paged_append(plan: Plan, cache: Cache, k, v, q=None, q_out=None, rope: Ro
                     stream=None):
     """k, v: [>=max_tokens, kv_heads, dim]; q, q_out: [>=max_tokens, q_heads, dim]
     (q_out may be q) or None."""
-    b = _fits(plan, cache)
+    dev = _device()
+    b = _fits(plan, cache, dev)
     n, dim = b.max_tokens, b.head_dim
     if (q is None) != (q_out is None):
         raise ValueError("q and q_out go together")
     if rope is not None and rope.handle is None:  # NULL would mean that nothing turns
         raise ValueError("the rotation has been freed")
-    vk, vv = _view(k, "k", n, b.kv_heads, dim), _view(v, "v", n, b.kv_heads, dim, k.dtype)
-    vq = _NO_VIEW if q is None else _view(q, "q", n, b.q_heads, dim, k.dtype)
-    vo = _NO_VIEW if q is None else _view(q_out, "q_out", n, b.q_heads, dim, k.dtype)
+    vk, vv = _view(k, "k", dev, n, b.kv_heads, dim), _view(v, "v", dev, n, b.kv_heads, dim, k.dtype)
+    vq = _NO_VIEW if q is None else _view(q, "q", dev, n, b.q_heads, dim, k.dtype)
+    vo = _NO_VIEW if q is None else _view(q_out, "q_out", dev, n, b.q_heads, dim, k.dtype)
     _check(LIB.kv_paged_append(plan.ref, cache.ref, None if rope is None else rope.handle,
-                               _dtype(k, "k"), vq, vo, vk, vv, _stream(stream)))
+                               _dtype(k, "k"), vq, vo, vk, vv, _stream(stream, dev)))
 
 
 def kv_paged_attention(plan: Plan, cache: Cache, q, out=None, lse=None, scale=None, stream=None):
     """q, out: [>=max_tokens, q_heads, dim]; lse: float32 [>=max_tokens, q_heads] or
     None; scale: dim ** -0.5 when None.  Returns out."""
-    b = _fits(plan, cache)
+    dev = _device()
+    b = _fits(plan, cache, dev)
     n, heads, dim = b.max_tokens, b.q_heads, b.head_dim
+    vq = _view(q, "q", dev, n, heads, dim)
     if out is None:
-        out = _output(q, (n, heads, dim), stream)
-    vq, vo = _view(q, "q", n, heads, dim), _view(out, "out", n, heads, dim, q.dtype)
-    pl = None if lse is None else _array(lse, "lse", torch.float32, n * heads)
+        out = _output(q, (n, heads, dim), stream, dev)
+    vo = _view(out, "out", dev, n, heads, dim, q.dtype)
+    pl = None if lse is None else _array(lse, "lse", dev, torch.float32, n * heads)
     _check(LIB.kv_paged_attention(plan.ref, cache.ref, _dtype(q, "q"), vq, vo, pl,
-                                  dim ** -0.5 if scale is None else scale, _stream(stream)))
+                                  dim ** -0.5 if scale is None else scale, _stream(stream, dev)))
     return out

@@ -55,6 +55,7 @@ def plan_for(K):
     p = K.Plan(2, 8, 16, 4, 4, 2, 64, device="cpu")
     for name in ("q_start", "kv_len", "slot", "pos", "result", "work"):
         setattr(p, name, on_gpu(getattr(p, name)))
+    p.dev = 0
     return p
 
 
@@ -148,4 +149,48 @@ def test_outputs_are_made_under_the_stream_that_writes_them(binding, places, str
     assert out.shape == x.shape and out.dtype == x.dtype and places == [where] and lib.calls[-1][1][-1] == handle
     out = K.kv_rope_apply(rope, x, on_gpu(torch.zeros(8, dtype=torch.int32)), stream=stream)
     assert out.shape == x.shape and out.dtype == x.dtype and places == [where] * 2 and lib.calls[-1][1][-1] == handle
+    rope.handle = None
+
+
+def test_tensors_of_another_device_are_refused(binding):
+    """Every tensor has to be on the current device, where the kernels run; so have the
+    plan, the cache and the stream."""
+    K, lib = binding
+    f16, i32 = dict(dtype=torch.float16), dict(dtype=torch.int32)
+    p = plan_for(K)
+    for at in range(4):
+        tensors = step()
+        tensors[at] = on_gpu(torch.Tensor(tensors[at]).to(torch.int32), 1)
+        with pytest.raises(ValueError, match="current device"):
+            K.kv_paged_plan(p, *tensors)
+    K.kv_paged_plan(p, *step())
+    x, kc, vc = torch.zeros(8, 4, 64, **f16), torch.zeros(3, 2, 16, 64, **f16), torch.zeros(3, 2, 64, 16, **f16)
+    cache = K.Cache(on_gpu(kc), on_gpu(vc))
+    rope = K.Rope.__new__(K.Rope)
+    rope.handle = 5
+    here, there, pos = on_gpu(x), on_gpu(x, 1), on_gpu(torch.zeros(8, **i32))
+    kv, kv_there = here[:, :2], on_gpu(x[:, :2], 1)
+    n = len(lib.calls)
+    elsewhere = plan_for(K)
+    K.kv_paged_plan(elsewhere, *step())
+    elsewhere.dev = 1
+    for bad in (lambda: K.kv_rope_apply(rope, there, pos, out=here), lambda: K.kv_rope_apply(rope, here, pos, out=there),
+                lambda: K.kv_rope_apply(rope, here, on_gpu(torch.zeros(8, **i32), 1), out=here),
+                lambda: K.kv_paged_append(p, cache, kv_there, kv), lambda: K.kv_paged_append(p, cache, kv, kv_there),
+                lambda: K.kv_paged_append(p, cache, kv, kv, q=there, q_out=here), lambda: K.kv_paged_append(p, cache, kv, kv, q=here, q_out=there),
+                lambda: K.kv_paged_attention(p, cache, there, out=here), lambda: K.kv_paged_attention(p, cache, here, out=there),
+                lambda: K.kv_paged_attention(p, cache, here, out=here, lse=on_gpu(torch.zeros(8, 4), 1)),
+                lambda: K.kv_paged_attention(p, K.Cache(on_gpu(kc, 1), on_gpu(vc, 1)), here, out=here),
+                lambda: K.Cache(on_gpu(kc), on_gpu(vc, 1)),
+                lambda: K.Cache(on_gpu(kc.to(torch.float8_e4m3fn)), on_gpu(vc.to(torch.float8_e4m3fn)), k_scale=on_gpu(torch.ones(2), 1)),
+                lambda: K.kv_paged_attention(elsewhere, cache, here, out=here),
+                lambda: K.kv_paged_plan(elsewhere, *step())):
+        with pytest.raises(ValueError, match="device"):
+            bad()
+    other = type("S", (), dict(cuda_stream=9, device_index=1))
+    for bad in (lambda: K.kv_paged_plan(p, *step(), stream=other), lambda: K.kv_paged_append(p, cache, kv, kv, stream=other),
+                lambda: K.kv_rope_apply(rope, here, pos, out=here, stream=other), lambda: K.kv_paged_attention(p, cache, here, out=here, stream=other)):
+        with pytest.raises(ValueError, match="device"):
+            bad()
+    assert len(lib.calls) == n + 1
     rope.handle = None
