@@ -124,6 +124,8 @@ def _view(t, name, dev, tokens, heads, dim, dtype=None):
     by_token, by_head, by_element = t.stride()
     if by_element != 1:
         raise ValueError(f"{name}: a head's elements must be contiguous")
+    if (by_token | by_head) & 7:  # refused by the library, but not for a dimension of one element
+        by_token, by_head = 0 if s[0] == 1 else by_token, 0 if s[1] == 1 else by_head
     return kv_heads_view(t.data_ptr(), by_token, by_head)
 
 
@@ -243,7 +245,8 @@ class Cache:
         n, heads, block, dim = k.shape
         if tuple(v.shape) != (n, heads, dim, block) or v.dtype != k.dtype or k.dtype not in _TYPES:
             raise ValueError(f"v has shape {tuple(v.shape)} and dtype {v.dtype}, k {tuple(k.shape)} and {k.dtype}")
-        if k.stride()[1:] != (block * dim, dim, 1) or v.stride()[1:] != (dim * block, block, 1):
+        # (by the first block: a dimension of one element may have any stride)
+        if not k[:1].is_contiguous() or not v[:1].is_contiguous():
             raise ValueError("a block of the cache must be contiguous")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.shape = (heads, block, dim)

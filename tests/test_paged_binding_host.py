@@ -194,3 +194,32 @@ def test_tensors_of_another_device_are_refused(binding):
             bad()
     assert len(lib.calls) == n + 1
     rope.handle = None
+
+
+def test_the_stride_of_one_element_says_nothing(binding):
+    """One token at an odd stride, and a cache of one key/value head whose blocks were
+    made token by token: each lies as the library needs it."""
+    K, lib = binding
+    f16, i32 = dict(dtype=torch.float16), dict(dtype=torch.int32)
+    rope = K.Rope.__new__(K.Rope)
+    rope.handle = 5
+    one = on_gpu(torch.zeros(400, **f16).as_strided((1, 4, 64), (259, 64, 1)))
+    assert one.stride(0) % 8
+    out = on_gpu(torch.zeros(1, 4, 64, **f16))
+    K.kv_rope_apply(rope, one, on_gpu(torch.zeros(1, **i32)), out=out)
+    vx, vy = lib.calls[-1][1][2:4]
+    assert vx.token_stride % 8 == 0 and vx.head_stride == 64 and vy.head_stride == 64
+    head = on_gpu(torch.zeros(400, **f16).as_strided((4, 1, 64), (64, 3, 1)))
+    K.kv_rope_apply(rope, head, on_gpu(torch.zeros(4, **i32)), out=on_gpu(torch.zeros(4, 1, 64, **f16)))
+    vx = lib.calls[-1][1][2]
+    assert vx.token_stride == 64 and vx.head_stride % 8 == 0
+    kc = on_gpu(torch.zeros(3, 16, 1, 64, **f16).transpose(1, 2))
+    vc = on_gpu(torch.zeros(3, 64, 1, 16, **f16).transpose(1, 2))
+    assert kc.stride(1) == 64 and vc.stride(1) == 16
+    c = K.Cache(kc, vc).c
+    assert (c.k_block_stride, c.v_block_stride, c.n_blocks) == (1024, 1024, 3)
+    for k, v in ((torch.zeros(3, 16, 2, 64, **f16).transpose(1, 2), torch.zeros(3, 2, 64, 16, **f16)),
+                 (torch.zeros(3, 2, 16, 64, **f16), torch.zeros(3, 2, 16, 64, **f16).transpose(2, 3))):
+        with pytest.raises(ValueError, match="contiguous"):
+            K.Cache(on_gpu(k), on_gpu(v))
+    rope.handle = None
