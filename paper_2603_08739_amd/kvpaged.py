@@ -15,6 +15,9 @@ is not the current one the rules are torch's: the inputs have to be ready on it,
 memory must not be given away before it is done with them, and an output that the call
 makes (out=None) belongs to it: the current stream waits for it before a use, and such
 a use is recorded (Tensor.record_stream) if the output may be dropped before it ends.
+
+kv_rope_apply takes part in automatic differentiation.  The other calls do not: what
+they write carries no gradient.
 """
 from __future__ import annotations
 
@@ -161,9 +164,7 @@ class Rope:
             pass
 
 
-def kv_rope_apply(rope: Rope, x, pos, out=None, backward=False, stream=None):
-    """x: [tokens, heads, dim] bfloat16 / float16 at any token and head stride;
-    pos: int32 [tokens]; out: like x (may be x), made when None.  Returns out."""
+def _rotate(rope, x, pos, out, backward, stream):
     dev = _device()
     n, heads, dim = x.shape
     vx = _view(x, "x", dev, n, heads, dim)
@@ -174,6 +175,45 @@ def kv_rope_apply(rope: Rope, x, pos, out=None, backward=False, stream=None):
                              _array(pos, "pos", dev, torch.int32, n), n, heads, dim,
                              1 if backward else 0, _stream(stream, dev)))
     return out
+
+
+class _Rotation(torch.autograd.Function):
+    """y = rotation of x; the gradient of x is that of y turned the other way."""
+
+    @staticmethod
+    def forward(ctx, x, rope, pos, backward, stream):
+        ctx.save_for_backward(pos)
+        ctx.rope, ctx.turned_back = rope, backward
+        return _rotate(rope, x, pos, None, backward, stream)
+
+    @staticmethod
+    def backward(ctx, grad):
+        pos, = ctx.saved_tensors
+        # gradients come expanded, transposed or from the inside of other tensors
+        if grad.data_ptr() % 16 or not grad.is_contiguous():
+            grad = grad.clone(memory_format=torch.contiguous_format)
+        return kv_rope_apply(ctx.rope, grad, pos, backward=not ctx.turned_back), None, None, None, None
+
+
+def kv_rope_apply(rope: Rope, x, pos, out=None, backward=False, stream=None):
+    """x: [tokens, heads, dim] bfloat16 / float16 at any token and head stride;
+    pos: int32 [tokens]; out: like x (may be x), made when None.  Returns out.
+
+    An x that requires a gradient gets one (rope and the values in pos are to be kept
+    until the backward pass); a given out then takes part as by out.copy_()."""
+    if x.requires_grad and torch.is_grad_enabled():
+        turned = _Rotation.apply(x, rope, pos, backward, stream)
+        if out is None:
+            return turned
+        _view(out, "out", _device(), *x.shape, x.dtype)
+        # on the stream that the call is for
+        if stream is None:
+            out[:x.shape[0]].copy_(turned)
+        else:
+            with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=x.device) if isinstance(stream, int) else stream):
+                out[:x.shape[0]].copy_(turned)
+        return out
+    return _rotate(rope, x, pos, out, backward, stream)
 
 
 class Plan:
