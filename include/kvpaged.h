@@ -71,7 +71,8 @@ typedef struct kv_rope_desc {
   double base;           /* > 1                                               */
   double factor;         /* LINEAR, BY_PARTS: >= 1                            */
   double fast, slow;     /* BY_PARTS: fast > slow >= 0                        */
-  double magnitude;      /* multiplies the turned elements; finite, nonzero   */
+  double magnitude;      /* multiplies the turned elements, in 32 bits: finite
+                            and nonzero there                                 */
 } kv_rope_desc;
 
 typedef struct kv_rope kv_rope; /* opaque: the pairs' frequencies, on the current device */

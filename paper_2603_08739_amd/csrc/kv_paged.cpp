@@ -113,7 +113,8 @@ extern "C" kv_status kv_rope_create(const kv_rope_desc* d, kv_rope** out) {
     if (d->layout > KV_ROPE_INTERLEAVED) return invalid(who, "unknown layout");
     if (d->scaling > KV_ROPE_BY_PARTS) return invalid(who, "unknown scaling");
     if (!(d->base > 1) || !std::isfinite(d->base)) return invalid(who, "base must be > 1 and finite");
-    if (!std::isfinite(d->magnitude) || d->magnitude == 0) return invalid(who, "magnitude must be finite and not 0");
+    // as the kernels hold it
+    if (!std::isfinite((float)d->magnitude) || (float)d->magnitude == 0) return invalid(who, "magnitude must be finite and not 0 in 32 bits");
     if (d->scaling != KV_ROPE_PLAIN && (!(d->factor >= 1) || !std::isfinite(d->factor))) return invalid(who, "factor must be >= 1 and finite");
     if (d->scaling == KV_ROPE_BY_PARTS && (!d->original_len || !(d->slow >= 0) || !(d->fast > d->slow) || !std::isfinite(d->fast)))
       return invalid(who, "BY_PARTS needs original_len > 0 and fast > slow >= 0");
