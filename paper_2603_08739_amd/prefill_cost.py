@@ -18,6 +18,7 @@ from __future__ import annotations
 
 import argparse
 import collections
+import itertools
 import json
 
 import numpy as np
@@ -45,17 +46,14 @@ class BlockPool:
         return run
 
     def take(self, n, pinned):
-        """n blocks for new contents, or None; none of `pinned` (hashes) is given away."""
-        out = []
-        while len(out) < n and self.free:
-            out.append(self.free.popleft())
-        if len(out) < n:
-            for h in [h for h in self.held if h not in pinned][:n - len(out)]:
-                out.append(self.held.pop(h))
-        if len(out) < n:
-            self.free.extend(out)
+        """n blocks for new contents; none of `pinned` (hashes) is given away.  None, and
+        nothing is given away, if there are not so many."""
+        old = max(0, n - len(self.free))
+        if old > len(self.held) - sum(h in self.held for h in pinned):
             return None
-        return out
+        out = [self.free.popleft() for _ in range(n - old)]
+        oldest = itertools.islice((h for h in self.held if h not in pinned), old)
+        return out + [self.held.pop(h) for h in list(oldest)]
 
     def keep(self, h, block):
         """`block` holds h from now on; given back if another block does already."""
