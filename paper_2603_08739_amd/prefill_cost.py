@@ -70,26 +70,31 @@ def requests_of(trace):
 
 
 def batches(trace, n_blocks, batch):
-    """Serving steps: (ctx blocks, new blocks, table rows, blocks taken) per batch.  A
+    """Serving steps: (cached blocks, blocks taken) of every request of a batch.  A
     request whose blocks are all cached computes its last one again: an answer
-    needs a token.  One that does not fit ends the batch; alone, it is skipped."""
+    needs a token.  One that does not fit the cache, or with which the step would bring
+    more new tokens than a plan takes, ends the batch; alone, it is skipped."""
     pool, waiting = BlockPool(n_blocks), collections.deque(requests_of(trace))
+    block = trace.tokens_per_granule * (int(trace.weight.max()) if len(trace.weight) else 1)
     while waiting:
         step, pinned, fresh = [], set(), []
+        room = kvpaged.KV_PAGED_MAX_TOKENS // block  # new blocks that the step may still bring
         while waiting and len(step) < batch:
             hashes = waiting[0]
             run = pool.prefix(hashes)[:len(hashes) - 1]
-            got = pool.take(len(hashes) - len(run), pinned | set(hashes[:len(run)]))
+            new = len(hashes) - len(run)
+            got = pool.take(new, pinned | set(hashes[:len(run)])) if new <= room else None
             if got is None:
                 if not step:
                     waiting.popleft()
                 break
             waiting.popleft()
+            room -= new
             pinned |= set(hashes[:len(run)])
             step.append((run, got))
             fresh += list(zip(hashes[len(run):], got))
-        for h, block in fresh:
-            pool.keep(h, block)
+        for h, block_of in fresh:
+            pool.keep(h, block_of)
         if step:
             yield step
 

@@ -31,3 +31,42 @@ def test_prefixes_survive_a_request_that_is_too_long():
         with_it = [step for step in batches(trace(short[:1] + [long] + short[1:]), 20, batch)]
         lens = [(len(run), len(got)) for step in with_it for run, got in step]
         assert lens[0] == (0, 8) and lens[1] == (8, 1)
+
+
+def documents(lengths, tokens=64):
+    """A trace of one request for each length (in blocks), no block shared."""
+    t = tg.from_blocks(np.arange(sum(lengths)))
+    t.req = np.repeat(np.arange(len(lengths)), lengths).astype(np.uint32)
+    t.tokens_per_granule = tokens
+    return t
+
+
+def test_a_step_brings_no_more_tokens_than_the_plan_takes():
+    """Document-sized requests: a batch ends before its new tokens pass what a step may
+    bring; a request that passes it alone is skipped."""
+    from paper_2603_08739_amd.kvpaged import KV_PAGED_MAX_TOKENS
+    from paper_2603_08739_amd.prefill_cost import batches
+    lengths = [2047] * 9 + [8192, 8193, 2000, 2000, 2000, 2192, 1]
+    t = documents(lengths)
+    steps = [[len(got) for _, got in step] for step in batches(t, 100_000, 16)]
+    assert all(64 * sum(s) <= KV_PAGED_MAX_TOKENS for s in steps)
+    assert steps == [[2047] * 4, [2047] * 4, [2047], [8192], [2000, 2000, 2000, 2192], [1]]
+
+
+def test_long_documents_of_the_workloads_fit():
+    from paper_2603_08739_amd.kvpaged import KV_PAGED_MAX_TOKENS
+    from paper_2603_08739_amd.prefill_cost import batches
+    t = tg.longctx(n_req=300, n_docs=40)
+    served = 0
+    for step in batches(t, 40_000, 16):
+        assert sum(len(got) for _, got in step) * t.tokens_per_granule <= KV_PAGED_MAX_TOKENS
+        served += len(step)
+    assert served == 300
+
+
+def test_steps_of_weighted_blocks():
+    """Blocks of four granules hold four times the tokens."""
+    from paper_2603_08739_amd.prefill_cost import batches
+    t = documents([5000, 3000, 3000], tokens=16)
+    t.weight[:] = 4
+    assert [[len(got) for _, got in s] for s in batches(t, 100_000, 16)] == [[5000, 3000], [3000]]
