@@ -138,7 +138,7 @@ def measure(trace, n_blocks, batch=16, max_requests=None, q_heads=32, kv_heads=8
             at[2].record()
             kvpaged.kv_paged_attention(plan, cache, q, out=out)
             at[3].record()
-        marks.append((at, plan))
+        marks.append((at, plan.result))  # not the plan: its work memory is tens of megabytes
         done["requests"] += len(step)
         done["steps"] += 1
         done["cached_tokens"] += sum(ctx)
@@ -146,9 +146,9 @@ def measure(trace, n_blocks, batch=16, max_requests=None, q_heads=32, kv_heads=8
         if max_requests is not None and done["requests"] >= max_requests:
             break
     torch.cuda.synchronize()
-    for at, plan in marks:
-        if plan.result[3].item():
-            raise RuntimeError(f"a step's plan was refused: {plan.result.tolist()}")
+    for at, result in marks:
+        if result[3].item():
+            raise RuntimeError(f"a step's plan was refused: {result.tolist()}")
         for i, name in enumerate(("plan_s", "append_s", "attention_s")):
             done[name] += at[i].elapsed_time(at[i + 1]) * 1e-3
     rope.free()
