@@ -113,10 +113,8 @@ def measure(trace, n_blocks, batch=16, max_requests=None, q_heads=32, kv_heads=8
     cache, rope = kvpaged.Cache(k, v), kvpaged.Rope(head_dim, base=base)
     i32 = dict(dtype=torch.int32, device=device)
     done = dict(requests=0, steps=0, cached_tokens=0, new_tokens=0, plan_s=0.0, append_s=0.0, attention_s=0.0)
-    marks = []
-    for step in batches(trace, n_blocks, batch):
-        if max_requests is not None:
-            step = step[:max_requests - done["requests"]]
+
+    def serve(step):  # one step's tensors are let go before the next one's are made
         ctx = [len(run) * block for run, _ in step]
         new = [len(got) * block for _, got in step]
         columns = max(len(run) + len(got) for run, got in step)
@@ -138,11 +136,17 @@ def measure(trace, n_blocks, batch=16, max_requests=None, q_heads=32, kv_heads=8
             at[2].record()
             kvpaged.kv_paged_attention(plan, cache, q, out=out)
             at[3].record()
-        marks.append((at, plan.result))  # not the plan: its work memory is tens of megabytes
         done["requests"] += len(step)
         done["steps"] += 1
         done["cached_tokens"] += sum(ctx)
         done["new_tokens"] += total
+        return at, plan.result  # not the plan: its work memory is tens of megabytes
+
+    marks = []
+    for step in batches(trace, n_blocks, batch):
+        if max_requests is not None:
+            step = step[:max_requests - done["requests"]]
+        marks.append(serve(step))
         if max_requests is not None and done["requests"] >= max_requests:
             break
     torch.cuda.synchronize()
