@@ -84,11 +84,9 @@ _raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDev
 
 
 def _stream(stream, dev):
-    """The stream's handle; None is the current stream of the current device `dev`.  These
-    calls take a few microseconds on the device, and torch.cuda.current_stream()
-    would take three more: the handle is asked for without making a Stream."""
-    if stream is None:
-        return _raw_stream(dev)
+    """The handle of a stream of the current device `dev`.  The current stream's is
+    _raw_stream(dev): these calls take a few microseconds on the device, and
+    torch.cuda.current_stream() would take three more."""
     if isinstance(stream, int):
         return stream
     if getattr(stream, "device_index", dev) != dev:
@@ -108,21 +106,25 @@ def _output(like, shape, stream, dev):
         return torch.empty(shape, dtype=like.dtype, device=like.device)
 
 
-def _dtype(t, name):
-    d = _TYPES.get(t.dtype)
-    if d is None or d == KV_DT_FP8:
-        raise ValueError(f"{name} has dtype {t.dtype}; expected bfloat16 or float16")
+_HEAD_TYPES = {torch.bfloat16: KV_DT_BF16, torch.float16: KV_DT_F16}
+
+
+def _dtype(dtype, name):
+    d = _HEAD_TYPES.get(dtype)
+    if d is None:
+        raise ValueError(f"{name} has dtype {dtype}; expected bfloat16 or float16")
     return d
 
 
-def _view(t, name, dev, tokens, heads, dim, dtype=None):
-    """[tokens, heads, dim] on device `dev` with contiguous elements, at least `tokens` rows."""
+def _view(t, name, dev, tokens, heads, dim, dtype):
+    """[tokens, heads, dim] of this dtype on device `dev`, with contiguous elements and at
+    least `tokens` rows."""
     if t.get_device() != dev:
         raise ValueError(f"{name} must be a CUDA tensor of the current device")
     s = t.shape
     if len(s) != 3 or s[0] < tokens or s[1] != heads or s[2] != dim:
         raise ValueError(f"{name} has shape {tuple(s)}; the call needs [>={tokens}, {heads}, {dim}]")
-    if dtype is not None and t.dtype is not dtype:
+    if t.dtype is not dtype:
         raise ValueError(f"{name} has dtype {t.dtype}; expected {dtype}")
     by_token, by_head, by_element = t.stride()
     if by_element != 1:
@@ -134,7 +136,7 @@ def _view(t, name, dev, tokens, heads, dim, dtype=None):
 
 def _array(t, name, dev, dtype, numel):
     """A contiguous tensor of this dtype on device `dev` with at least `numel` elements."""
-    if t.get_device() != dev or t.dtype != dtype or not t.is_contiguous() or t.numel() < numel:
+    if t.get_device() != dev or t.dtype is not dtype or not t.is_contiguous() or t.numel() < numel:
         raise ValueError(f"{name} must be a contiguous CUDA {dtype} tensor of the current device, of at least {numel} elements")
     return t.data_ptr()
 
@@ -164,19 +166,6 @@ class Rope:
             pass
 
 
-def _rotate(rope, x, pos, out, backward, stream):
-    dev = _device()
-    n, heads, dim = x.shape
-    vx = _view(x, "x", dev, n, heads, dim)
-    if out is None:
-        out = _output(x, (n, heads, dim), stream, dev)
-    vy = _view(out, "out", dev, n, heads, dim, x.dtype)
-    _check(LIB.kv_rope_apply(rope.handle, _dtype(x, "x"), vx, vy,
-                             _array(pos, "pos", dev, torch.int32, n), n, heads, dim,
-                             1 if backward else 0, _stream(stream, dev)))
-    return out
-
-
 class _Rotation(torch.autograd.Function):
     """y = rotation of x; the gradient of x is that of y turned the other way."""
 
@@ -184,7 +173,7 @@ class _Rotation(torch.autograd.Function):
     def forward(ctx, x, rope, pos, backward, stream):
         ctx.save_for_backward(pos)
         ctx.rope, ctx.turned_back = rope, backward
-        return _rotate(rope, x, pos, None, backward, stream)
+        return kv_rope_apply(rope, x, pos, backward=backward, stream=stream)  # recording is off in here
 
     @staticmethod
     def backward(ctx, grad):
@@ -195,6 +184,19 @@ class _Rotation(torch.autograd.Function):
         return kv_rope_apply(ctx.rope, grad, pos, backward=not ctx.turned_back), None, None, None, None
 
 
+def _recorded_rotation(rope, x, pos, out, backward, stream):
+    turned = _Rotation.apply(x, rope, pos, backward, stream)
+    if out is None:
+        return turned
+    _view(out, "out", _device(), *x.shape, x.dtype)
+    if stream is None:
+        out[:x.shape[0]].copy_(turned)
+    else:
+        with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=x.device) if isinstance(stream, int) else stream):
+            out[:x.shape[0]].copy_(turned)
+    return out
+
+
 def kv_rope_apply(rope: Rope, x, pos, out=None, backward=False, stream=None):
     """x: [tokens, heads, dim] bfloat16 / float16 at any token and head stride;
     pos: int32 [tokens]; out: like x (may be x), made when None.  Returns out.
@@ -202,18 +204,16 @@ def kv_rope_apply(rope: Rope, x, pos, out=None, backward=False, stream=None):
     An x that requires a gradient gets one (rope and the values in pos are to be kept
     until the backward pass); a given out then takes part as by out.copy_()."""
     if x.requires_grad and torch.is_grad_enabled():
-        turned = _Rotation.apply(x, rope, pos, backward, stream)
-        if out is None:
-            return turned
-        _view(out, "out", _device(), *x.shape, x.dtype)
-        # on the stream that the call is for
-        if stream is None:
-            out[:x.shape[0]].copy_(turned)
-        else:
-            with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=x.device) if isinstance(stream, int) else stream):
-                out[:x.shape[0]].copy_(turned)
-        return out
-    return _rotate(rope, x, pos, out, backward, stream)
+        return _recorded_rotation(rope, x, pos, out, backward, stream)
+    dev, dtype = _device(), x.dtype
+    n, heads, dim = x.shape
+    kind, vx = _dtype(dtype, "x"), _view(x, "x", dev, n, heads, dim, dtype)
+    if out is None:
+        out = _output(x, (n, heads, dim), stream, dev)
+    vy = vx if out is x else _view(out, "out", dev, n, heads, dim, dtype)
+    _check(LIB.kv_rope_apply(rope.handle, kind, vx, vy, _array(pos, "pos", dev, torch.int32, n), n, heads, dim,
+                             1 if backward else 0, _raw_stream(dev) if stream is None else _stream(stream, dev)))
+    return out
 
 
 class Plan:
@@ -252,16 +252,17 @@ def kv_paged_plan(plan: Plan, ctx_len, new_len, table, free_list=None, stream=No
     b, dev = plan.batch, _device()
     if plan.dev != dev:
         raise ValueError(f"the plan is on device {plan.dev}; the current device is {dev}")
-    if table.dim() != 2 or table.shape[1] != b.max_blocks:
-        raise ValueError(f"table has shape {tuple(table.shape)}; the plan's rows have {b.max_blocks} blocks")
+    n, columns, shape = b.n_req, b.max_blocks, table.shape
+    if len(shape) != 2 or shape[1] != columns:
+        raise ValueError(f"table has shape {tuple(shape)}; the plan's rows have {columns} blocks")
     i32 = torch.int32
     # all of it is checked before the batch points at any of it: after a refusal the
     # batch is that of the step planned before, whose tensors are kept
-    step = (_array(ctx_len, "ctx_len", dev, i32, b.n_req), _array(new_len, "new_len", dev, i32, b.n_req),
-            _array(table, "table", dev, i32, b.n_req * b.max_blocks), 0 if free_list is None else free_list.numel(),
+    step = (_array(ctx_len, "ctx_len", dev, i32, n), _array(new_len, "new_len", dev, i32, n),
+            _array(table, "table", dev, i32, n * columns), 0 if free_list is None else free_list.numel(),
             # an empty tensor has no address, and NULL would mean that table names every block
             None if free_list is None else _array(free_list, "free_list", dev, i32, 0) or b.result)
-    stream = _stream(stream, dev)
+    stream = _raw_stream(dev) if stream is None else _stream(stream, dev)
     b.ctx_len, b.new_len, b.table, b.n_free, b.free_list = step
     try:
         _check(LIB.kv_paged_plan(plan.ref, stream))
@@ -302,6 +303,7 @@ class Cache:
 
 
 def _fits(plan, cache, dev):
+    """The batch and its number of tokens; the cache has the plan's shape."""
     b = plan.batch
     if plan.dev != dev or cache.dev != dev:
         raise ValueError(f"the plan is on device {plan.dev}, the cache on {cache.dev}; the current device is {dev}")
@@ -310,7 +312,7 @@ def _fits(plan, cache, dev):
                          f"the plan's {(b.kv_heads, b.block_size, b.head_dim)}")
     if plan.inputs is None:
         raise ValueError("the plan is empty: call kv_paged_plan first")
-    return b
+    return b, b.max_tokens
 
 
 def kv_paged_append(plan: Plan, cache: Cache, k, v, q=None, q_out=None, rope: Rope | None = None,
@@ -318,30 +320,35 @@ def kv_paged_append(plan: Plan, cache: Cache, k, v, q=None, q_out=None, rope: Ro
     """k, v: [>=max_tokens, kv_heads, dim]; q, q_out: [>=max_tokens, q_heads, dim]
     (q_out may be q) or None."""
     dev = _device()
-    b = _fits(plan, cache, dev)
-    n, dim = b.max_tokens, b.head_dim
+    b, n = _fits(plan, cache, dev)
+    heads, _, dim = cache.shape
+    dtype = k.dtype
     if (q is None) != (q_out is None):
         raise ValueError("q and q_out go together")
     if rope is not None and rope.handle is None:  # NULL would mean that nothing turns
         raise ValueError("the rotation has been freed")
-    vk, vv = _view(k, "k", dev, n, b.kv_heads, dim), _view(v, "v", dev, n, b.kv_heads, dim, k.dtype)
-    vq = _NO_VIEW if q is None else _view(q, "q", dev, n, b.q_heads, dim, k.dtype)
-    vo = _NO_VIEW if q is None else _view(q_out, "q_out", dev, n, b.q_heads, dim, k.dtype)
-    _check(LIB.kv_paged_append(plan.ref, cache.ref, None if rope is None else rope.handle,
-                               _dtype(k, "k"), vq, vo, vk, vv, _stream(stream, dev)))
+    kind, vk, vv = _dtype(dtype, "k"), _view(k, "k", dev, n, heads, dim, dtype), _view(v, "v", dev, n, heads, dim, dtype)
+    if q is None:
+        vq = vo = _NO_VIEW
+    else:
+        heads = b.q_heads
+        vq = _view(q, "q", dev, n, heads, dim, dtype)
+        vo = vq if q_out is q else _view(q_out, "q_out", dev, n, heads, dim, dtype)
+    _check(LIB.kv_paged_append(plan.ref, cache.ref, None if rope is None else rope.handle, kind, vq, vo, vk, vv,
+                               _raw_stream(dev) if stream is None else _stream(stream, dev)))
 
 
 def kv_paged_attention(plan: Plan, cache: Cache, q, out=None, lse=None, scale=None, stream=None):
     """q, out: [>=max_tokens, q_heads, dim]; lse: float32 [>=max_tokens, q_heads] or
     None; scale: dim ** -0.5 when None.  Returns out."""
     dev = _device()
-    b = _fits(plan, cache, dev)
-    n, heads, dim = b.max_tokens, b.q_heads, b.head_dim
-    vq = _view(q, "q", dev, n, heads, dim)
+    b, n = _fits(plan, cache, dev)
+    heads, dim, dtype = b.q_heads, cache.shape[2], q.dtype
+    kind, vq = _dtype(dtype, "q"), _view(q, "q", dev, n, heads, dim, dtype)
     if out is None:
         out = _output(q, (n, heads, dim), stream, dev)
-    vo = _view(out, "out", dev, n, heads, dim, q.dtype)
+    vo = _view(out, "out", dev, n, heads, dim, dtype)
     pl = None if lse is None else _array(lse, "lse", dev, torch.float32, n * heads)
-    _check(LIB.kv_paged_attention(plan.ref, cache.ref, _dtype(q, "q"), vq, vo, pl,
-                                  dim ** -0.5 if scale is None else scale, _stream(stream, dev)))
+    _check(LIB.kv_paged_attention(plan.ref, cache.ref, kind, vq, vo, pl, dim ** -0.5 if scale is None else scale,
+                                  _raw_stream(dev) if stream is None else _stream(stream, dev)))
     return out
