@@ -185,7 +185,10 @@ def main(argv=None):
     _, obj = host.evaluate(handle, cfgs, dict(tg.DEFAULT_COST, t_prefill_per_token=t), trace.n_groups)
     handle.free()
     flags, n = host.pareto(obj)
-    print(json.dumps({**{k: round(v, 6) for k, v in done.items()}, "t_prefill_per_token": t, "configs": int(cfgs.n), "front": int(n)}))
+    holds = "attention and the cache's upkeep, measured; " + (
+        "the products with the weights as given by --other-us" if a.other_us else "without the products with the weights (--other-us)")
+    print(json.dumps({**{k: round(v, 6) for k, v in done.items()}, "layers": a.layers, "other_s_per_token": a.other_us * 1e-6,
+                      "t_prefill_per_token": t, "t_prefill_per_token_holds": holds, "configs": int(cfgs.n), "front": int(n)}))
     return done, t, obj, flags
 
 
