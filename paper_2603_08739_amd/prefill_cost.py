@@ -105,6 +105,8 @@ def measure(trace, n_blocks, batch=16, max_requests=None, q_heads=32, kv_heads=8
     weights = np.unique(trace.weight)
     if len(weights) != 1:
         raise ValueError("the requests' blocks must have one size")
+    if max_requests is not None and max_requests < 1:
+        raise ValueError("max_requests must be at least 1")
     block = int(trace.tokens_per_granule * weights[0])
     g = torch.Generator(device=device)
     g.manual_seed(seed)
