@@ -96,8 +96,9 @@ typedef struct kv_heads_view {
 /* y = rotation of x at positions pos, per pair (a, b) with angle p*f_i and
  * magnitude m: (m*(a*cos - b*sin), m*(a*sin + b*cos)); backward: the same with
  * the angle negated, the gradient of x for a gradient of y.  Elements past
- * rot_dim are copied.  Angles are reduced modulo a turn exactly (64 bits of
- * the frequency), the products are in 32 bits, rounded once.
+ * rot_dim are copied.  Frequencies have the 53 bits of a double and angles are
+ * reduced modulo a turn without further error: they are off by less than 2^-22
+ * turns at any position.  The products are in 32 bits, rounded once.
  *   dtype     KV_DT_BF16 or KV_DT_F16
  *   x, y      views; y may be x itself (same pointer and strides), otherwise
  *             they must not overlap
@@ -209,7 +210,9 @@ kv_status kv_paged_append(const kv_paged_batch* b, const kv_paged_cache* c, cons
  * (no other: as if nothing was seen), one of +inf or NaN leaves NaN in out and
  * lse.  Products are on the matrix cores with 32-bit sums; softmax statistics
  * are in 32 bits; the weights are rounded to the queries' type for the second
- * product.  Results do not depend on timing.
+ * product.  Sums are taken with weights of up to 2^14 before the division, so
+ * values past some 10^30 may leave the 32-bit range.  Results do not depend on
+ * timing.
  *   q, out    views of q_heads heads; out must not overlap q (the
  *             same pointer is KV_ERR_INVALID)
  *   lse       device float [max_tokens][q_heads] or NULL

@@ -165,12 +165,16 @@ __device__ __forceinline__ float element(const uint8_t* p) {
 //
 // One prompt of 8,111 tokens after 256 cached ones, 32 query and 8 key/value heads of
 // 128, bf16: 573 GFLOP over the keys that queries see in 557 to 619 us (cards
-// differ), 0.93 to 1.03 PFLOP/s where a large matrix product does 1.3 to 1.4.  The matrix
+// differ), 0.93 to 1.03 PFLOP/s where a large matrix product does 1.3 to 1.4; on a card
+// that has rested before each call 630, under a kernel trace up to 690.  The matrix
 // cores are busy half of the time: the exponentials, conversions and masks take
-// vector instructions, of which two wavefronts on a SIMD hide a part only.  Heads of
-// 64: 870 TFLOP/s, heads of 256: 700.  What was tried beside it and was no faster: the
-// next scores worked out between the steps of the softmax (599 us for 577), LDS
-// reads issued a step ahead (740, registers spilled), wavefront priorities (the same).
+// vector instructions, of which two wavefronts on a SIMD hide a part only.  The same
+// prompt over an 8-bit cache: 579 us beside 571.  Heads of 64: 885 TFLOP/s, 8 bits the
+// same; half of the products for each exponential.  Heads of 256: 685, 8 bits 770; one
+// wavefront on a SIMD has the registers, so that nothing hides its softmax.  What was
+// tried beside it and was no faster: the next scores worked out between the steps of
+// the softmax (599 us for 577), LDS reads issued a step ahead (740, registers spilled),
+// wavefront priorities (the same).
 template <int D, int kBytes>
 struct TileLds {
   static constexpr int kRowChunks = D * kBytes / 16;              // of a row of K

@@ -327,8 +327,8 @@ kv_status paged_plan(const kv_paged_batch& b, const WorkLayout& w, hipStream_t s
   a.split = (SplitTile*)(at + w.split);
   a.done = (uint32_t*)(at + w.done);
   // Threads of a workgroup: few requests and tiles are done in one round of 256, whose
-  // barriers are the cheaper ones (a step of 64 chats: 7.4 us a call, 8.8 with 1,024
-  // threads); more of them need the threads (1,000 ragged prompts: 15.6 us, 26.7 with 256).
+  // barriers are the cheaper ones (a step of 64 chats: 6.0 us a call, 7.0 with 1,024
+  // threads); more of them need the threads (1,000 ragged prompts: 10.0 us, 22.9 with 256).
   const uint32_t threads = b.n_req <= 256 && w.max_tiles <= 512 ? 256 : 1024;
   const uint32_t grid = 1 + (b.max_tokens + 4 * threads - 1) / (4 * threads);
   // three arrays of n_req and two ends: at most 49 KB

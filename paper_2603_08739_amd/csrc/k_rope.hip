@@ -1,12 +1,13 @@
 // k_rope.hip - rotary positions, and the write of a step's keys and values
 // into a paged cache.
 //
-// A pair (a, b) of a head at position p turns by the angle p*f.  The angle is
-// kept as a fraction of a turn in 64 fixed-point bits, so that p*f modulo a
-// turn is one wrapping product, exact to p*2^-64 turns at any position (in
-// 32-bit floating point p*f itself is off by 0.004 radians at p = 131,072).  The
-// sine and cosine of the remaining eighth of a turn are Taylor sums whose next
-// term is below 2^-25.
+// A pair (a, b) of a head at position p turns by the angle p*f.  f is kept as a
+// fraction of a turn in 64 fixed-point bits, so that p*f modulo a turn is one
+// wrapping product without rounding.  What remains is the error of f itself, which
+// is worked out in double: a few units of 2^-53 of at most 0.16 turns, less than
+// 2^-22 turns at any 32-bit position (in 32-bit floating point p*f is off by 0.004
+// radians at p = 131,072 already).  The sine and cosine of the remaining eighth of a
+// turn are Taylor sums whose next term is below 2^-25.
 //
 // All of it is bound by memory traffic and, at a step's few tokens, by latency.
 // A thread owns 16 elements of a head (8 pairs: two 16-byte loads and stores,
