@@ -11,10 +11,11 @@ serving step is
 
 Tensors, plan, cache and rotation are on the current device.  Calls go to the current
 stream, or to `stream`: a torch.cuda.Stream or a stream's handle.  With a stream that
-is not the current one the rules are torch's: the inputs have to be ready on it, their
-memory must not be given away before it is done with them, and an output that the call
-makes (out=None) belongs to it: the current stream waits for it before a use, and such
-a use is recorded (Tensor.record_stream) if the output may be dropped before it ends.
+is not the current one the rules are torch's: inputs, plan and cache have to be ready
+on it, their memory must not be given away before it is done with them, and an output
+that the call makes (out=None) belongs to it: the current stream waits for it before a
+use, and such a use is recorded (Tensor.record_stream) if the output may be dropped
+before it ends.
 
 kv_rope_apply takes part in automatic differentiation.  The other calls do not: what
 they write carries no gradient.
