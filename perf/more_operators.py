@@ -204,7 +204,7 @@ def prepare(case, seed):
     if own:
         from paper_2603_08739_amd import kvpaged
         s["plan"] = kvpaged.Plan(reqs, max(total, 1), block, width, q_heads, kv_heads, dim, max_new=max(s["longest_new"], 1), window=c.get("window", 0))
-        s["cache"] = kvpaged.Cache(s["k_cache"], s["v_cache"], k_scale=s["k_scale"], v_scale=s["v_scale"])
+        s["cache"] = kvpaged.Cache(s["k_cache"], s["v_cache"], k_scale=s["k_scale"], v_scale=s["v_scale"], block_scales=True)
         s["rope"] = kvpaged.Rope(c["rot"], base=BASE, layout=c["layout"]) if c["op"] == "write" else None
         kvpaged.kv_paged_plan(s["plan"], s["ctx"], s["new"], s["table"])
     return s
