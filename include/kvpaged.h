@@ -14,6 +14,7 @@
  *                       written into the cache
  *   kv_paged_attention  attention of the step's new tokens over their
  *                       requests' blocks, single tokens and long chunks alike
+ *   kv_paged_read       tokens read back from the cache into rows of 16 bits
  *
  * Conventions are those of kvcfg.h: KV_OK or a negative kv_status with
  * kv_last_error(), arguments checked before any device work, no C++ exception
@@ -39,10 +40,15 @@
 extern "C" {
 #endif
 
-/* Element types.  KV_DT_FP8 (e4m3: 4 exponent bits, 3 mantissa bits, no
- * infinities, largest 448) is a cache type only: the value is the stored
- * number times the scale of its key/value head. */
-enum { KV_DT_BF16 = 0, KV_DT_F16 = 1, KV_DT_FP8 = 2 };
+/* Element types.  Those of 8 bits are cache types only; a held number stands for
+ * itself times a scale:
+ *   KV_DT_FP8        e4m3 (4 exponent bits, 3 mantissa bits, no infinities,
+ *                    largest 448); the scale of its key/value head, given by the
+ *                    caller
+ *   KV_DT_FP8_BLOCK  e4m3; the scale of its block and key/value head, which
+ *                    kv_paged_append finds and writes
+ *   KV_DT_I8_BLOCK   whole numbers -127..127 in two's complement; the same */
+enum { KV_DT_BF16 = 0, KV_DT_F16 = 1, KV_DT_FP8 = 2, KV_DT_FP8_BLOCK = 4, KV_DT_I8_BLOCK = 5 };
 
 enum {
   KV_PAGED_MAX_REQ = 4096,       /* requests of a step                        */
@@ -183,7 +189,12 @@ typedef struct kv_paged_cache {
   int64_t v_block_stride;
   uint32_t n_blocks;     /* >= 1                                              */
   uint32_t dtype;        /* KV_DT_*                                           */
-  const float* k_scale;  /* device [kv_heads], > 0: KV_DT_FP8 only; NULL = 1  */
+  const float* k_scale;  /* device; KV_DT_FP8: [kv_heads], > 0, NULL = 1;
+                            KV_DT_FP8_BLOCK, KV_DT_I8_BLOCK: [n_blocks][kv_heads],
+                            written by kv_paged_append (memory that may be
+                            written, whatever this pointer says); a caller that
+                            fills blocks itself gives scales >= 0, 0 for a block
+                            of zeros                                          */
   const float* v_scale;
 } kv_paged_cache;
 
@@ -197,10 +208,37 @@ typedef struct kv_paged_cache {
  * Into a KV_DT_FP8 cache goes value/scale rounded to nearest even, values past
  * +-448 as +-448, NaN as NaN.  Tokens without a slot, or with one outside the
  * cache, are not written; rows past the step's last token are left alone.  No
- * two tokens may have one slot. */
+ * two tokens may have one slot.
+ *
+ * Into a cache with scales by block, Q the type's largest number (448 or 127): of
+ * the new values in a block and head let need = max |value| / Q, infinities and NaN
+ * left out.  The scale s becomes need where the block's first token is among
+ * them.  A block that a context ends in keeps its scale, doubled n times until
+ * s >= need; its earlier numbers are then held as their 2^-n, rounded to nearest
+ * even.  (With nothing but zeros so far the scale is 0, and becomes need.)  The
+ * values are held as value * (1/s) in 32 bits, rounded to nearest even, past +-Q
+ * as +-Q; NaN as NaN in e4m3 and 0 as a whole number.  A block is written for one
+ * request of a step: requests that share the block a context ends in copy it first,
+ * scales too.  Nothing else of the cache is touched. */
 kv_status kv_paged_append(const kv_paged_batch* b, const kv_paged_cache* c, const kv_rope* rope,
                           uint32_t dtype, kv_heads_view q, kv_heads_view q_out, kv_heads_view k,
                           kv_heads_view v, void* stream);
+
+/* Reads tokens back: row i = row_start[r] .. row_start[r+1] - 1 of request r gets the
+ * key and value at position first[r] + i - row_start[r], times its scale, rounded
+ * once to dtype (16-bit caches: copied).  Positions that are not in the cache
+ * (negative, at or past kv_len, in a block that is not there) give zeros.  Rows past
+ * row_start[n_req] are left alone, as are rows past max_rows.
+ *   dtype      of k and v: KV_DT_BF16 or KV_DT_F16, a 16-bit cache's own
+ *   row_start  device int32 [n_req+1], not descending, from 0 on
+ *   first      device int32 [n_req], or NULL: 0
+ *   max_rows   rows of k and v: at most 2^31 - 1; 0 is a no-op
+ *   k, v       views of kv_heads heads; must not overlap each other or the cache
+ * Of the batch, sizes, table and kv_len are read: it has to be planned, and what is
+ * read to be written. */
+kv_status kv_paged_read(const kv_paged_batch* b, const kv_paged_cache* c, uint32_t dtype,
+                        const int32_t* row_start, const int32_t* first, uint32_t max_rows,
+                        kv_heads_view k, kv_heads_view v, void* stream);
 
 /* out[t][h] = sum_j softmax_j(scale * q[t][h].K[j]) V[j] over the keys j that
  * token t sees: its request's positions up to its own, within the window, in
@@ -209,8 +247,10 @@ kv_status kv_paged_append(const kv_paged_batch* b, const kv_paged_cache* c, cons
  * nothing whatever they hold.  Of what is seen, a score of -inf weighs nothing
  * (no other: as if nothing was seen), one of +inf or NaN leaves NaN in out and
  * lse.  Products are on the matrix cores with 32-bit sums; softmax statistics
- * are in 32 bits; the weights are rounded to the queries' type for the second
- * product.  Sums are taken with weights of up to 2^14 before the division, so
+ * are in 32 bits; the weights, times the values' scales by block relative to a power
+ * of two near the largest, are rounded to the queries' type for the second
+ * product (in float16, values in blocks whose scale is below 2^-20 of the largest
+ * that a request's queries see lose precision).  Sums are taken with weights of up to 2^14 before the division, so
  * values past some 10^30 may leave the 32-bit range.  Results do not depend on
  * timing.
  *   q, out    views of q_heads heads; out must not overlap q (the

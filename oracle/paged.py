@@ -102,3 +102,71 @@ def attention(q, k_cache, v_cache, table, q_start, ctx, block, n_blocks, scale, 
             lse[t] = torch.logsumexp(s, -1).reshape(H)
             reach[t] = (scale * (x.abs() @ kj.abs())).amax(-1).reshape(H)
     return out, lse, spread, reach
+
+
+# ---- a cache of 8 bits with a scale for each block and head ----
+
+MOST = {"fp8": 448.0, "i8": 127.0}
+
+
+def held(x, kind):
+    """The held numbers nearest to x (float64, in units of the scale), ties to even."""
+    y = torch.nan_to_num(x, nan=math.nan, posinf=MOST[kind], neginf=-MOST[kind]).clamp(-MOST[kind], MOST[kind])
+    if kind == "i8":
+        return torch.nan_to_num(y, nan=0.0).round()
+    step = torch.exp2(torch.floor(torch.log2(y.abs().clamp(min=2.0 ** -6))) - 3)   # 3 bits below the first, 2^-9 at the least
+    return (y / step).round() * step
+
+
+def rises(need, old):
+    """The least n >= 0 with need <= old * 2^n."""
+    n = 0
+    while need > old * 2.0 ** n:
+        n += 1
+    return n
+
+
+def write_blocks(x, numbers, scale, table, q_start, ctx, block, n_blocks, kind):
+    """A step's values x [T, J, D] float64 into numbers [n_blocks, J, block, D] and scale
+    [n_blocks, J], float64, both changed; lists elsewhere.  Returns the (block, place) of
+    every token, or None for one that is not written."""
+    places = [None] * q_start[-1]
+    for r in range(len(ctx)):
+        t, end = q_start[r], q_start[r + 1]
+        while t < end:
+            at = (ctx[r] + t - q_start[r]) % block
+            n = min(block - at, end - t)
+            page = table[r][(ctx[r] + t - q_start[r]) // block]
+            if 0 <= page < n_blocks:
+                for j in range(x.shape[1]):
+                    new = x[t:t + n, j]
+                    size = new[torch.isfinite(new)].abs()
+                    need = float(size.max()) / MOST[kind] if size.numel() else 0.0
+                    old = float(scale[page, j]) if at else 0.0
+                    if not (0.0 < old < math.inf):
+                        if at and need > 0:
+                            numbers[page, j, :at] = held(numbers[page, j, :at] * 0.0, kind)
+                        scale[page, j] = need
+                    else:
+                        m = rises(need, old)
+                        numbers[page, j, :at] = held(numbers[page, j, :at] * 2.0 ** -m, kind) if m else numbers[page, j, :at]
+                        scale[page, j] = old * 2.0 ** m
+                    s = float(scale[page, j])
+                    numbers[page, j, at:at + n] = held(new / s if s else torch.where(torch.isinf(new), new, new * 0.0), kind)
+                for i in range(n):
+                    places[t + i] = (page, at + i)
+            t += n
+    return places
+
+
+def read_rows(numbers, scale, table, kv_len, block, n_blocks, starts, first):
+    """Rows [starts[-1], J, D] float64 of numbers [n_blocks, J, block, D] times scale
+    [n_blocks, J]."""
+    rows = torch.zeros(starts[-1], numbers.shape[1], numbers.shape[3], dtype=torch.float64)
+    for r in range(len(kv_len)):
+        for i in range(starts[r], starts[r + 1]):
+            p = first[r] + i - starts[r]
+            page = table[r][p // block] if 0 <= p < kv_len[r] else -1
+            if 0 <= page < n_blocks:
+                rows[i] = numbers[page, :, p % block] * scale[page][:, None]
+    return rows

@@ -1,0 +1,469 @@
+// k_block.hip - the write of a step's keys and values into a paged cache of 8 bits with a
+// scale for each block of tokens and head, and the read of any paged cache into rows.
+//
+// A held number c of block b and head h stands for c * s[b][h].  With Q the type's
+// largest number and x what a step puts into the block, need = max |x| / Q:
+//   the block's first token is among them:  s = need
+//   it goes on (a context ends inside it):  s = old * 2^n, the least n >= 0 with
+//                                           need <= s; earlier numbers become
+//                                           round(c * 2^-n)
+// and c = round(x * (1 / s)).  Scales rise by whole powers of two, so that the
+// earlier numbers' roundings add up to less than one unit whatever the number of rises
+// (1/2 + 1/4 + ...), where scales that follow the maximum would add half a unit each time.
+//
+// Both kernels walk over runs: the tokens of one request in one block.  A workgroup
+// takes a run of one head.  No two runs of a step write to one block, so there is
+// no order among workgroups, and no atomics.
+#include "rope_device.h"
+
+namespace kv {
+using namespace rope;
+namespace {
+
+// ---------------------------------------------------------------------------
+// runs
+// ---------------------------------------------------------------------------
+// Request r has tokens start[r] .. start[r+1] - 1 of a packed batch, at positions
+// from `at` on.  They fall into at most n / size + 2 blocks, so the places
+// start[r] / size + 2 r  and on are its own; some stay empty.  A place finds its
+// request by a search over r, 64 candidates at a time.  Where requests times the runs
+// that one can have is about as many places (single tokens, one long prompt),
+// those are used and nothing is searched.
+struct Runs {
+  const int32_t* start;  // [n_req + 1]
+  uint32_t n_req, shift;
+  uint32_t each;         // runs of a request, or 0: search
+};
+
+uint64_t plan_runs(Runs& r, const int32_t* start, uint32_t n_req, uint32_t block, uint64_t tokens, uint64_t most) {
+  r.start = start, r.n_req = n_req, r.shift = (uint32_t)__builtin_ctz(block);
+  const uint64_t found = tokens / block + 2ull * n_req;
+  const uint64_t one = most <= 1 ? 1 : (most - 1) / block + 2;
+  const bool direct = one * n_req <= 2 * found && one * n_req <= 0xffffffffull;
+  r.each = direct ? (uint32_t)one : 0;
+  return direct ? one * n_req : found;
+}
+
+// The request of place u and which of its runs it is; the whole wavefront asks.
+__device__ __forceinline__ void find_run(const Runs& runs, uint32_t u, uint32_t& req, uint32_t& run) {
+  if (runs.each) {
+    req = u / runs.each;
+    run = u - req * runs.each;
+    return;
+  }
+  auto base = [&](uint32_t r) { return ((uint32_t)max(runs.start[r], 0) >> runs.shift) + 2 * r; };
+  uint32_t lo = 0, n = runs.n_req;
+  while (n > 1) {
+    const uint32_t step = (n + 63) / 64, at = lane_id() * step;
+    const uint64_t below = __ballot(at < n && base(lo + min(at, n - 1)) <= u);
+    const uint32_t i = (uint32_t)max((int)__popcll(below) - 1, 0) * step;
+    lo += i;
+    n = min(step, n - i);
+  }
+  const uint32_t mine = base(lo);
+  req = mine <= u ? lo : runs.n_req;  // (a first row that is not 0 leaves the places before it to nobody)
+  run = u - mine;
+}
+
+// ---------------------------------------------------------------------------
+// the two held types
+// ---------------------------------------------------------------------------
+struct Fp8 {
+  static constexpr float kMost = 448.0f;
+  static __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) { return pack_fp8x4(a, b, c, d); }
+  template <int I>
+  static __device__ __forceinline__ float value(uint32_t u) { return __builtin_amdgcn_cvt_f32_fp8((int)u, I); }
+};
+struct I8 {
+  static constexpr float kMost = 127.0f;
+  // nearest even: the low bits of a sum with 3 * 2^22 are the whole number
+  static __device__ __forceinline__ uint32_t bits(float x) {
+    x = x == x ? x : 0.0f;
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_fmed3f(x, -127.0f, 127.0f) + 12582912.0f);
+  }
+  static __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
+    const uint32_t lo = __builtin_amdgcn_perm(bits(b), bits(a), 0x0c0c0400u);
+    const uint32_t hi = __builtin_amdgcn_perm(bits(d), bits(c), 0x04000c0cu);
+    return lo | hi;
+  }
+  template <int I>
+  static __device__ __forceinline__ float value(uint32_t u) { return (float)(int8_t)(u >> (8 * I)); }
+};
+
+template <class H>
+__device__ __forceinline__ void values4(uint32_t u, float* f) {
+  f[0] = H::template value<0>(u), f[1] = H::template value<1>(u), f[2] = H::template value<2>(u), f[3] = H::template value<3>(u);
+}
+// earlier numbers in a larger unit
+template <class H>
+__device__ __forceinline__ uint32_t shrink4(uint32_t u, float by) {
+  float f[4];
+  values4<H>(u, f);
+  return H::pack4(f[0] * by, f[1] * by, f[2] * by, f[3] * by);
+}
+
+// Infinities and NaN do not make a scale.
+__device__ __forceinline__ float magnitude_of(float x) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x) & 0x7fffffffu;
+  return __builtin_bit_cast(float, u < 0x7f800000u ? u : 0u);
+}
+
+struct NewScale {
+  float scale, inverse, shrink;  // shrink: of the earlier numbers
+};
+// `old`: the scale so far, 0 for a block that begins.  What no write has left there (NaN,
+// infinities, negative and subnormal numbers) counts as 0.
+__device__ __forceinline__ NewScale new_scale(float need, float old) {
+  NewScale n;
+  n.shrink = 1.0f;
+  n.scale = need;
+  if (old >= 0x1p-126f && old <= 3.402823466e38f) {
+    const uint32_t a = __builtin_bit_cast(uint32_t, need), b = __builtin_bit_cast(uint32_t, old);
+    int rise = 0;
+    if (need > old) {
+      rise = (int)(a >> 23) - (int)(b >> 23) + ((a & 0x7fffffu) > (b & 0x7fffffu) ? 1 : 0);
+      n.shrink = __builtin_amdgcn_ldexpf(1.0f, -rise);
+    }
+    n.scale = __builtin_amdgcn_ldexpf(old, rise);
+  } else if (need > 0.0f) {
+    n.shrink = 0.0f;
+  }
+  // (any number does for zeros; infinities become the largest number with this one)
+  n.inverse = n.scale > 0.0f ? 1.0f / n.scale : 0x1p-126f;
+  return n;
+}
+
+// ---------------------------------------------------------------------------
+// the write
+// ---------------------------------------------------------------------------
+struct BlockArgs {
+  Runs runs;
+  const uint64_t* turn;
+  const int32_t *pos, *kv_len;
+  const int64_t* slot;
+  const uint16_t *q, *k, *v;
+  uint16_t* q_out;
+  int64_t qt, qh, ot, oh, kt, kh, vt, vh;
+  uint8_t *kc, *vc;
+  int64_t k_block, v_block;
+  float *k_scale, *v_scale;
+  uint64_t slots;  // n_blocks * block_size
+  uint32_t max_tokens, q_heads, kv_heads, dim, units, rot_dim, heads_each, q_groups;
+  uint32_t q_blocks;  // workgroups of queries; the rest take runs
+  float magnitude;
+};
+
+constexpr int kStrip = 64;  // elements of V turned through LDS at a time
+
+template <class V, bool kHalf, class H>
+__global__ __launch_bounds__(256) void k_append_block(BlockArgs a) {
+  const int tid = threadIdx.x;
+  if (blockIdx.x < a.q_blocks) {  // queries: as in k_append
+    const uint32_t n_tokens = min((uint32_t)max(a.runs.start[a.runs.n_req], 0), a.max_tokens);
+    const uint64_t id = (uint64_t)blockIdx.x * 256 + tid;
+    const uint32_t unit = (uint32_t)(id % a.units);
+    const uint64_t rest = id / a.units;
+    const uint32_t group = (uint32_t)(rest % a.q_groups);
+    const uint64_t token = rest / a.q_groups;
+    if (token >= n_tokens) return;
+    const bool turns = unit < a.rot_dim / 16;
+    Turns t;
+    if (turns) load_turns(t, a.turn, unit, a.pos[token], 1.0f, a.magnitude);
+    int lo, hi;
+    unit_at<kHalf>(unit, a.rot_dim, lo, hi);
+    turn_heads<V, kHalf>(a.q + (int64_t)token * a.qt, a.qh, a.q_out + (int64_t)token * a.ot, a.oh, group * a.heads_each,
+                         min(a.q_heads, (group + 1) * a.heads_each), lo, hi, turns, t);
+    return;
+  }
+
+  const uint32_t id = blockIdx.x - a.q_blocks, head = id % a.kv_heads;
+  uint32_t req, run;
+  find_run(a.runs, id / a.kv_heads, req, run);
+  if (req >= a.runs.n_req) return;
+  const int64_t size = 1ll << a.runs.shift;
+  const int64_t t0 = a.runs.start[req], t1 = min((int64_t)a.runs.start[req + 1], (int64_t)a.max_tokens);
+  if (t0 < 0 || t0 >= t1) return;
+  // the run: n tokens from `token` on, in places `at` and on of their block
+  const int64_t ctx = a.kv_len[req] - ((int64_t)a.runs.start[req + 1] - t0);
+  if (ctx < 0) return;
+  const int64_t block0 = ((ctx >> a.runs.shift) + run) << a.runs.shift;
+  const int64_t from = max(ctx, block0), to = min(ctx + (t1 - t0), block0 + size);
+  if (from >= to) return;
+  const uint32_t token = (uint32_t)(t0 + (from - ctx)), n = (uint32_t)(to - from), at = (uint32_t)(from - block0);
+  const int64_t slot = a.slot[token];
+  if (slot < 0 || (uint64_t)slot >= a.slots) return;
+  const int64_t page = slot >> a.runs.shift;
+
+  const uint16_t* k = a.k + (int64_t)token * a.kt + head * a.kh;
+  const uint16_t* v = a.v + (int64_t)token * a.vt + head * a.vh;
+  // a thread's 16 elements of a key: item = token * units + unit
+  auto key = [&](uint32_t item, float* f, float* g, int& lo, int& hi) {
+    const uint32_t t = item / a.units, unit = item - t * a.units;
+    unit_at<kHalf>(unit, a.rot_dim, lo, hi);
+    const uint16_t* p = k + (int64_t)t * a.kt;
+    unpack<V>(*(const uint4*)(p + lo), f);
+    unpack<V>(*(const uint4*)(p + hi), g);
+    if (unit < a.rot_dim / 16) {
+      Turns turns;
+      load_turns(turns, a.turn, unit, a.pos[token + t], 1.0f, a.magnitude);
+      turn_unit<kHalf>(f, g, turns);
+    }
+    return t;
+  };
+
+  // the largest magnitudes
+  float most_k = 0.0f, most_v = 0.0f;
+  for (uint32_t item = tid; item < n * a.units; item += 256) {
+    float f[8], g[8];
+    int lo, hi;
+    key(item, f, g, lo, hi);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) most_k = fmaxf(most_k, fmaxf(magnitude_of(f[i]), magnitude_of(g[i])));
+  }
+  for (uint32_t item = tid; item < n * a.units * 2; item += 256) {
+    const uint32_t t = item / (a.units * 2), chunk = item - t * a.units * 2;
+    float f[8];
+    unpack<V>(*(const uint4*)(v + (int64_t)t * a.vt + chunk * 8), f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) most_v = fmaxf(most_v, magnitude_of(f[i]));
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) most_k = fmaxf(most_k, __shfl_xor(most_k, d, 64)), most_v = fmaxf(most_v, __shfl_xor(most_v, d, 64));
+  __shared__ float most[2][4];
+  if (lane_id() == 0) most[0][wave_id()] = most_k, most[1][wave_id()] = most_v;
+  const int64_t scale_at = page * a.kv_heads + head;
+  const float old_k = at ? a.k_scale[scale_at] : 0.0f, old_v = at ? a.v_scale[scale_at] : 0.0f;
+  __syncthreads();
+  // A need that is not 0 is no subnormal number: new_scale() reads exponents.
+  auto need = [&](const float* m) {
+    const float x = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) / H::kMost;
+    return x > 0.0f ? fmaxf(x, 0x1p-126f) : 0.0f;
+  };
+  const NewScale sk = new_scale(need(most[0]), old_k), sv = new_scale(need(most[1]), old_v);
+  if (tid == 0) a.k_scale[scale_at] = sk.scale, a.v_scale[scale_at] = sv.scale;
+
+  // keys
+  uint8_t* kc = a.kc + page * a.k_block + ((int64_t)head << a.runs.shift) * a.dim;
+  for (uint32_t item = tid; item < n * a.units; item += 256) {
+    float f[8], g[8];
+    int lo, hi;
+    const uint32_t t = key(item, f, g, lo, hi);
+    uint8_t* to_row = kc + (int64_t)(at + t) * a.dim;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] *= sk.inverse, g[i] *= sk.inverse;
+    *(uint2*)(to_row + lo) = make_uint2(H::pack4(f[0], f[1], f[2], f[3]), H::pack4(f[4], f[5], f[6], f[7]));
+    *(uint2*)(to_row + hi) = make_uint2(H::pack4(g[0], g[1], g[2], g[3]), H::pack4(g[4], g[5], g[6], g[7]));
+  }
+  if (at && sk.shrink != 1.0f)
+    for (uint32_t i = tid; i < at * a.dim / 4; i += 256) {
+      uint32_t* p = (uint32_t*)kc + i;
+      *p = shrink4<H>(*p, sk.shrink);
+    }
+
+  // values: a strip of elements through LDS, then along the tokens
+  uint8_t* vc = a.vc + page * a.v_block + ((int64_t)head * a.dim << a.runs.shift);
+  __shared__ uint8_t strip[kStrip][256 + 4];
+  for (uint32_t d0 = 0; d0 < a.dim; d0 += kStrip) {
+    __syncthreads();
+    for (uint32_t item = tid; item < n * (kStrip / 8); item += 256) {
+      const uint32_t t = item / (kStrip / 8), chunk = item % (kStrip / 8);
+      float f[8];
+      unpack<V>(*(const uint4*)(v + (int64_t)t * a.vt + d0 + chunk * 8), f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] *= sv.inverse;
+      const uint32_t lo = H::pack4(f[0], f[1], f[2], f[3]), hi = H::pack4(f[4], f[5], f[6], f[7]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) strip[chunk * 8 + i][t] = (uint8_t)(lo >> (8 * i)), strip[chunk * 8 + 4 + i][t] = (uint8_t)(hi >> (8 * i));
+    }
+    __syncthreads();
+    for (uint32_t i = tid; i < n * kStrip; i += 256) {
+      const uint32_t d = i / n, t = i - d * n;
+      vc[((int64_t)(d0 + d) << a.runs.shift) + at + t] = strip[d][t];
+    }
+  }
+  if (at && sv.shrink != 1.0f)
+    for (uint32_t i = tid; i < at * a.dim; i += 256) {
+      const uint32_t d = i / at, t = i - d * at;
+      uint8_t* p = vc + ((int64_t)d << a.runs.shift) + t;
+      *p = (uint8_t)shrink4<H>(*p, sv.shrink);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// the read
+// ---------------------------------------------------------------------------
+struct ReadArgs {
+  Runs runs;
+  const int32_t *first, *table, *kv_len;
+  uint16_t *k, *v;
+  int64_t kt, kh, vt, vh;
+  const uint8_t *kc, *vc;
+  int64_t k_block, v_block;  // bytes
+  const float *k_scale, *v_scale;
+  uint32_t max_rows, max_blocks, n_blocks, kv_heads, dim;
+  uint32_t by_block;  // scales by block, or by head
+};
+
+// held types of the read: 16 bits too
+struct Same {};
+
+template <class V, class H>
+__global__ __launch_bounds__(256) void k_read(ReadArgs a) {
+  constexpr int kBytes = __is_same(H, Same) ? 2 : 1;
+  const int tid = threadIdx.x;
+  const uint32_t head = blockIdx.x % a.kv_heads;
+  uint32_t req, run;
+  find_run(a.runs, blockIdx.x / a.kv_heads, req, run);
+  if (req >= a.runs.n_req) return;
+  const int64_t size = 1ll << a.runs.shift;
+  const int64_t t0 = a.runs.start[req], t1 = min((int64_t)a.runs.start[req + 1], (int64_t)a.max_rows);
+  if (t0 < 0 || t0 >= t1) return;
+  const int64_t first = a.first ? a.first[req] : 0;
+  const int64_t block0 = ((first >> a.runs.shift) + run) << a.runs.shift;
+  const int64_t from = max(first, block0), to = min(first + (t1 - t0), block0 + size);
+  if (from >= to) return;
+  const uint32_t row = (uint32_t)(t0 + (from - first)), n = (uint32_t)(to - from), at = (uint32_t)(from - block0);
+  // rows that are in the cache: the block's first tokens, or none
+  const int64_t column = block0 >> a.runs.shift;
+  int page = -1;
+  if (column >= 0 && column < a.max_blocks) page = a.table[(uint64_t)req * a.max_blocks + column];
+  const int64_t end = page >= 0 && page < (int)a.n_blocks ? min((int64_t)a.kv_len[req], to) : from;
+  const uint32_t have = (uint32_t)max(end - from, (int64_t)0);
+  page = have ? page : 0;
+
+  float ks = 1.0f, vs = 1.0f;
+  if constexpr (kBytes == 1) {
+    const int64_t i = (a.by_block ? (int64_t)page * a.kv_heads : 0) + head;
+    if (a.k_scale) ks = a.k_scale[i];
+    if (a.v_scale) vs = a.v_scale[i];
+  }
+  uint16_t* k = a.k + (int64_t)row * a.kt + head * a.kh;
+  uint16_t* v = a.v + (int64_t)row * a.vt + head * a.vh;
+  const uint8_t* kc = a.kc + page * a.k_block + (((int64_t)head << a.runs.shift) + at) * a.dim * kBytes;
+  const uint8_t* vc = a.vc + page * a.v_block + ((int64_t)head * a.dim << a.runs.shift) * kBytes;
+  const uint32_t chunks = a.dim / 8;
+  for (uint32_t i = tid; i < n * chunks; i += 256) {
+    const uint32_t t = i / chunks, c = i - t * chunks;
+    uint4 u = make_uint4(0, 0, 0, 0);
+    if (t < have) {
+      if constexpr (kBytes == 2) {
+        u = *(const uint4*)(kc + ((int64_t)t * a.dim + c * 8) * 2);
+      } else {
+        const uint2 w = *(const uint2*)(kc + (int64_t)t * a.dim + c * 8);
+        float f[8];
+        values4<H>(w.x, f);
+        values4<H>(w.y, f + 4);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] *= ks;
+        u = pack<V>(f);
+      }
+    }
+    *(uint4*)(k + (int64_t)t * a.kt + c * 8) = u;
+  }
+  // values: a strip of elements through LDS
+  __shared__ uint16_t strip[256][kStrip + 8];
+  for (uint32_t d0 = 0; d0 < a.dim; d0 += kStrip) {
+    __syncthreads();
+    for (uint32_t i = tid; i < n * kStrip; i += 256) {
+      const uint32_t d = i / n, t = i - d * n;
+      uint16_t u = 0;
+      if (t < have) {
+        const uint8_t* p = vc + (((int64_t)(d0 + d) << a.runs.shift) + at + t) * kBytes;
+        if constexpr (kBytes == 2) {
+          u = *(const uint16_t*)p;
+        } else {
+          u = __builtin_bit_cast(uint16_t, (typename Elem<V>::type)(H::template value<0>(*p) * vs));
+        }
+      }
+      strip[t][d] = u;
+    }
+    __syncthreads();
+    for (uint32_t i = tid; i < n * (kStrip / 8); i += 256) {
+      const uint32_t t = i / (kStrip / 8), c = i % (kStrip / 8);
+      *(uint4*)(v + (int64_t)t * a.vt + d0 + c * 8) = *(const uint4*)&strip[t][c * 8];
+    }
+  }
+}
+
+template <class V, class H>
+void launch_append(const BlockArgs& a, bool half, uint32_t grid, hipStream_t s) {
+  if (half)
+    hipLaunchKernelGGL((k_append_block<V, true, H>), dim3(grid), dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((k_append_block<V, false, H>), dim3(grid), dim3(256), 0, s, a);
+}
+
+template <class V>
+void launch_read(const ReadArgs& a, uint32_t kept, uint32_t grid, hipStream_t s) {
+  if (kept == KV_DT_I8_BLOCK)
+    hipLaunchKernelGGL((k_read<V, I8>), dim3(grid), dim3(256), 0, s, a);
+  else if (eight_bits(kept))
+    hipLaunchKernelGGL((k_read<V, Fp8>), dim3(grid), dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((k_read<V, Same>), dim3(grid), dim3(256), 0, s, a);
+}
+
+}  // namespace
+
+kv_status paged_append_block(const kv_paged_batch& b, const kv_paged_cache& c, const RopeTable* r, uint32_t dtype,
+                             const kv_heads_view& q, const kv_heads_view& q_out, const kv_heads_view& k,
+                             const kv_heads_view& v, hipStream_t s) {
+  BlockArgs a{};
+  a.turn = r ? r->turn : nullptr;
+  a.rot_dim = r ? r->rot_dim : 0;
+  a.magnitude = r ? r->magnitude : 1.0f;
+  a.pos = b.pos, a.kv_len = b.kv_len, a.slot = b.slot;
+  a.q = (const uint16_t*)q.ptr, a.k = (const uint16_t*)k.ptr, a.v = (const uint16_t*)v.ptr;
+  a.q_out = (uint16_t*)q_out.ptr;
+  a.qt = q.token_stride, a.qh = q.head_stride, a.ot = q_out.token_stride, a.oh = q_out.head_stride;
+  a.kt = k.token_stride, a.kh = k.head_stride, a.vt = v.token_stride, a.vh = v.head_stride;
+  a.kc = (uint8_t*)c.k, a.vc = (uint8_t*)c.v;
+  a.k_block = c.k_block_stride, a.v_block = c.v_block_stride;
+  // written here and nowhere else: caches of this kind have their scales in memory that may be
+  a.k_scale = const_cast<float*>(c.k_scale), a.v_scale = const_cast<float*>(c.v_scale);
+  a.slots = (uint64_t)c.n_blocks * b.block_size;
+  a.max_tokens = b.max_tokens;
+  a.q_heads = q.ptr ? b.q_heads : 0, a.kv_heads = b.kv_heads;
+  a.dim = b.head_dim, a.units = b.head_dim / 16;
+  a.heads_each = heads_each_for((uint64_t)b.max_tokens * a.q_heads * a.units);
+  a.q_groups = (a.q_heads + a.heads_each - 1) / a.heads_each;
+  const uint64_t qs = ((uint64_t)b.max_tokens * a.q_groups * a.units + 255) / 256;
+  const uint64_t runs = plan_runs(a.runs, b.q_start, b.n_req, b.block_size, b.max_tokens,
+                                  b.max_new ? std::min(b.max_new, b.max_tokens) : b.max_tokens) * b.kv_heads;
+  if (qs + runs > 0x7fffffffull) return fail(KV_ERR_UNSUPPORTED, "kv_paged_append: too many heads for one call");
+  a.q_blocks = (uint32_t)qs;
+  const uint32_t grid = (uint32_t)(qs + runs);
+  const bool half = !r || r->layout == KV_ROPE_HALF, i8 = c.dtype == KV_DT_I8_BLOCK;
+  if (dtype == KV_DT_BF16)
+    i8 ? launch_append<bf16x8, I8>(a, half, grid, s) : launch_append<bf16x8, Fp8>(a, half, grid, s);
+  else
+    i8 ? launch_append<f16x8, I8>(a, half, grid, s) : launch_append<f16x8, Fp8>(a, half, grid, s);
+  KV_HIP(hipGetLastError());
+  return KV_OK;
+}
+
+kv_status paged_read(const kv_paged_batch& b, const kv_paged_cache& c, uint32_t dtype, const int32_t* row_start,
+                     const int32_t* first, uint32_t max_rows, const kv_heads_view& k, const kv_heads_view& v,
+                     hipStream_t s) {
+  const int bytes = eight_bits(c.dtype) ? 1 : 2;
+  ReadArgs a{};
+  a.first = first, a.table = b.table, a.kv_len = b.kv_len;
+  a.k = (uint16_t*)k.ptr, a.v = (uint16_t*)v.ptr;
+  a.kt = k.token_stride, a.kh = k.head_stride, a.vt = v.token_stride, a.vh = v.head_stride;
+  a.kc = (const uint8_t*)c.k, a.vc = (const uint8_t*)c.v;
+  a.k_block = c.k_block_stride * bytes, a.v_block = c.v_block_stride * bytes;
+  a.k_scale = c.k_scale, a.v_scale = c.v_scale;
+  a.by_block = by_block(c.dtype);
+  a.max_rows = max_rows, a.max_blocks = b.max_blocks, a.n_blocks = c.n_blocks;
+  a.kv_heads = b.kv_heads, a.dim = b.head_dim;
+  const uint64_t grid = plan_runs(a.runs, row_start, b.n_req, b.block_size, max_rows, max_rows) * b.kv_heads;
+  if (grid > 0x7fffffffull) return fail(KV_ERR_UNSUPPORTED, "kv_paged_read: too many rows for one call");
+  if (dtype == KV_DT_BF16)
+    launch_read<bf16x8>(a, c.dtype, (uint32_t)grid, s);
+  else
+    launch_read<f16x8>(a, c.dtype, (uint32_t)grid, s);
+  KV_HIP(hipGetLastError());
+  return KV_OK;
+}
+
+}  // namespace kv

@@ -90,8 +90,9 @@ const char* check_cache(const kv_paged_cache& c, const kv_paged_batch& b, uint32
     if (st < block || st % 16) return "a block stride is below a block's elements or no multiple of 16";
   if (c.n_blocks < 1 || c.n_blocks > (1u << 30)) return "n_blocks out of range";
   if (dtype != KV_DT_BF16 && dtype != KV_DT_F16) return "dtype must be KV_DT_BF16 or KV_DT_F16";
-  if (c.dtype != KV_DT_FP8 && c.dtype != dtype) return "the cache's dtype must be KV_DT_FP8 or that of the heads";
-  if (c.dtype != KV_DT_FP8 && (c.k_scale || c.v_scale)) return "scales belong to a KV_DT_FP8 cache";
+  if (!eight_bits(c.dtype) && c.dtype != dtype) return "the cache's dtype must be one of 8 bits or that of the heads";
+  if (!eight_bits(c.dtype) && (c.k_scale || c.v_scale)) return "scales belong to a cache of 8 bits";
+  if (by_block(c.dtype) && (!c.k_scale || !c.v_scale)) return "a cache with scales by block needs both scale arrays";
   if (!aligned(c.k_scale, 4) || !aligned(c.v_scale, 4)) return "a scale array is misaligned";
   return nullptr;
 }
@@ -230,7 +231,27 @@ extern "C" kv_status kv_paged_append(const kv_paged_batch* b, const kv_paged_cac
       if (const char* e = kv::check_view(q)) return invalid(who, e);
       if (const char* e = kv::check_view(q_out)) return invalid(who, e);
     }
+    if (kv::by_block(c->dtype))
+      return kv::paged_append_block(*b, *c, rope ? &rope->table : nullptr, dtype, q, q_out, k, v, (hipStream_t)stream);
     return kv::paged_append(*b, *c, rope ? &rope->table : nullptr, dtype, q, q_out, k, v, (hipStream_t)stream);
+  });
+}
+
+extern "C" kv_status kv_paged_read(const kv_paged_batch* b, const kv_paged_cache* c, uint32_t dtype, const int32_t* row_start,
+                                   const int32_t* first, uint32_t max_rows, kv_heads_view k, kv_heads_view v, void* stream) {
+  const char* who = "kv_paged_read";
+  return guarded(who, [&]() -> kv_status {
+    if (!b || !c) return invalid(who, "batch or cache is NULL");
+    if (const char* e = kv::check_batch(*b)) return invalid(who, e);
+    if (const char* e = kv::check_cache(*c, *b, dtype)) return invalid(who, e);
+    if (!row_start || !kv::aligned(row_start, 4)) return invalid(who, "row_start is NULL or misaligned");
+    if (!kv::aligned(first, 4)) return invalid(who, "first is misaligned");
+    if (max_rows > 0x7fffffffu) return invalid(who, "max_rows out of range");
+    if (max_rows == 0) return KV_OK;
+    if (const char* e = kv::check_view(k)) return invalid(who, e);
+    if (const char* e = kv::check_view(v)) return invalid(who, e);
+    if (k.ptr == v.ptr) return invalid(who, "k and v must not be the same");
+    return kv::paged_read(*b, *c, dtype, row_start, first, max_rows, k, v, (hipStream_t)stream);
   });
 }
 

@@ -118,6 +118,10 @@ inline WorkLayout work_layout(const kv_paged_batch& b) {
   return w;
 }
 
+// Scales by block of tokens and head, written with what they scale.
+inline bool by_block(uint32_t kept) { return kept == KV_DT_FP8_BLOCK || kept == KV_DT_I8_BLOCK; }
+inline bool eight_bits(uint32_t kept) { return kept == KV_DT_FP8 || by_block(kept); }
+
 // The frequencies of a rotation, in 2^-64 turns a token.
 struct RopeTable {
   const uint64_t* turn = nullptr;  // device [rot_dim / 2]
@@ -133,6 +137,13 @@ kv_status paged_plan(const kv_paged_batch& b, const WorkLayout& w, hipStream_t s
 kv_status paged_append(const kv_paged_batch& b, const kv_paged_cache& c, const RopeTable* r,
                        uint32_t dtype, const kv_heads_view& q, const kv_heads_view& q_out,
                        const kv_heads_view& k, const kv_heads_view& v, hipStream_t s);
+// c of KV_DT_FP8_BLOCK or KV_DT_I8_BLOCK
+kv_status paged_append_block(const kv_paged_batch& b, const kv_paged_cache& c, const RopeTable* r,
+                             uint32_t dtype, const kv_heads_view& q, const kv_heads_view& q_out,
+                             const kv_heads_view& k, const kv_heads_view& v, hipStream_t s);
+kv_status paged_read(const kv_paged_batch& b, const kv_paged_cache& c, uint32_t dtype,
+                     const int32_t* row_start, const int32_t* first, uint32_t max_rows,
+                     const kv_heads_view& k, const kv_heads_view& v, hipStream_t s);
 kv_status paged_attention(const kv_paged_batch& b, const WorkLayout& w, const kv_paged_cache& c,
                           uint32_t dtype, const kv_heads_view& q, const kv_heads_view& out,
                           float* lse, float scale, hipStream_t s);

@@ -9,6 +9,8 @@ serving step is
     kv_paged_append(plan, cache, k, v, q=q, q_out=q, rope=rope)      # every layer
     kv_paged_attention(plan, cache, q, out=out)
 
+and kv_paged_read(plan, cache, row_start, ...) gives tokens of the cache back as rows.
+
 Tensors, plan, cache and rotation are on the current device.  Calls go to the current
 stream, or to `stream`: a torch.cuda.Stream or a stream's handle.  With a stream that
 is not the current one the rules are torch's: inputs, plan and cache have to be ready
@@ -28,7 +30,7 @@ import torch
 
 from .kvcfg import KV_ERR_INVALID, KV_ERR_UNSUPPORTED, KV_OK, LIB, KvError, _check, kv_last_error  # noqa: F401
 
-KV_DT_BF16, KV_DT_F16, KV_DT_FP8 = 0, 1, 2
+KV_DT_BF16, KV_DT_F16, KV_DT_FP8, KV_DT_FP8_BLOCK, KV_DT_I8_BLOCK = 0, 1, 2, 4, 5
 KV_ROPE_HALF, KV_ROPE_INTERLEAVED = 0, 1
 KV_ROPE_PLAIN, KV_ROPE_LINEAR, KV_ROPE_BY_PARTS = 0, 1, 2
 KV_PLAN_BAD_LENGTH, KV_PLAN_TOKENS, KV_PLAN_BLOCKS = 1, 2, 4
@@ -62,7 +64,7 @@ class kv_paged_cache(ctypes.Structure):
 
 
 EXPORTS = ("kv_rope_create", "kv_rope_free", "kv_rope_apply", "kv_paged_work_bytes",
-           "kv_paged_plan", "kv_paged_append", "kv_paged_attention")
+           "kv_paged_plan", "kv_paged_append", "kv_paged_read", "kv_paged_attention")
 
 _P = ctypes.POINTER
 LIB.kv_rope_create.argtypes = [_P(kv_rope_desc), _P(_vp)]
@@ -73,6 +75,8 @@ LIB.kv_paged_work_bytes.argtypes = [_P(kv_paged_batch), _P(_u64)]
 LIB.kv_paged_plan.argtypes = [_P(kv_paged_batch), _vp]
 LIB.kv_paged_append.argtypes = [_P(kv_paged_batch), _P(kv_paged_cache), _vp, _u32, kv_heads_view,
                                 kv_heads_view, kv_heads_view, kv_heads_view, _vp]
+LIB.kv_paged_read.argtypes = [_P(kv_paged_batch), _P(kv_paged_cache), _u32, _vp, _vp, _u32, kv_heads_view,
+                              kv_heads_view, _vp]
 LIB.kv_paged_attention.argtypes = [_P(kv_paged_batch), _P(kv_paged_cache), _u32, kv_heads_view,
                                    kv_heads_view, _vp, ctypes.c_float, _vp]
 for _name in EXPORTS:
@@ -80,6 +84,7 @@ for _name in EXPORTS:
 
 
 _TYPES = {torch.bfloat16: KV_DT_BF16, torch.float16: KV_DT_F16, torch.float8_e4m3fn: KV_DT_FP8}
+_BLOCK_TYPES = {torch.float8_e4m3fn: KV_DT_FP8_BLOCK, torch.int8: KV_DT_I8_BLOCK}
 _NO_VIEW = kv_heads_view()
 _raw_stream, _device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
@@ -95,16 +100,16 @@ def _stream(stream, dev):
     return stream.cuda_stream
 
 
-def _output(like, shape, stream, dev):
-    """An output of `like`'s type, made under the stream that will write it: the memory
+def _output(like, shape, stream, dev, dtype=None):
+    """An output of `like`'s type (or `dtype`), made under the stream that will write it: the memory
     is then none that another stream may still be working on, and is not given to
     another stream while this one writes."""
     if stream is None or _stream(stream, dev) == _raw_stream(dev):
-        return torch.empty(shape, dtype=like.dtype, device=like.device)
+        return torch.empty(shape, dtype=dtype or like.dtype, device=like.device)
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream, device=like.device)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=like.dtype, device=like.device)
+        return torch.empty(shape, dtype=dtype or like.dtype, device=like.device)
 
 
 _HEAD_TYPES = {torch.bfloat16: KV_DT_BF16, torch.float16: KV_DT_F16}
@@ -276,16 +281,21 @@ def kv_paged_plan(plan: Plan, ctx_len, new_len, table, free_list=None, stream=No
 class Cache:
     """A layer's cache: k [n_blocks, kv_heads, block_size, head_dim], v [n_blocks,
     kv_heads, head_dim, block_size]; blocks may lie at any stride, each block is
-    contiguous.  float8_e4m3fn caches take k_scale, v_scale: float32 [kv_heads]."""
+    contiguous.  float8_e4m3fn caches take k_scale, v_scale: float32 [kv_heads].
 
-    def __init__(self, k, v, k_scale=None, v_scale=None):
+    With block_scales, k_scale and v_scale are float32 [n_blocks, kv_heads], a scale for
+    each block and head, and kv_paged_append writes them; k and v are int8 or
+    float8_e4m3fn.  The contents of a new cache do not matter."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None, block_scales=False):
         if k.dim() != 4 or v.dim() != 4 or not k.is_cuda or not v.is_cuda:
             raise ValueError("k and v must be CUDA tensors of four dimensions")
         dev = self.dev = k.get_device()
         if v.get_device() != dev:
             raise ValueError("k and v must be on one device")
         n, heads, block, dim = k.shape
-        if tuple(v.shape) != (n, heads, dim, block) or v.dtype != k.dtype or k.dtype not in _TYPES:
+        types = _BLOCK_TYPES if block_scales else _TYPES
+        if tuple(v.shape) != (n, heads, dim, block) or v.dtype != k.dtype or k.dtype not in types:
             raise ValueError(f"v has shape {tuple(v.shape)} and dtype {v.dtype}, k {tuple(k.shape)} and {k.dtype}")
         # (by the first block: a dimension of one element may have any stride)
         if not k[:1].is_contiguous() or not v[:1].is_contiguous():
@@ -297,7 +307,12 @@ class Cache:
         c.k, c.v = k.data_ptr(), v.data_ptr()
         c.k_block_stride = k.stride(0) if n > 1 else one
         c.v_block_stride = v.stride(0) if n > 1 else one
-        c.n_blocks, c.dtype = n, _TYPES[k.dtype]
+        c.n_blocks, c.dtype = n, types[k.dtype]
+        if block_scales:
+            for name, s in (("k_scale", k_scale), ("v_scale", v_scale)):
+                if s is None or tuple(s.shape) != (n, heads):
+                    raise ValueError(f"{name} must have shape {(n, heads)}: a scale for each block and head")
+            heads *= n
         c.k_scale = None if k_scale is None else _array(k_scale, "k_scale", dev, torch.float32, heads)
         c.v_scale = None if v_scale is None else _array(v_scale, "v_scale", dev, torch.float32, heads)
         self.ref = ctypes.byref(c)
@@ -337,6 +352,36 @@ def kv_paged_append(plan: Plan, cache: Cache, k, v, q=None, q_out=None, rope: Ro
         vo = vq if q_out is q else _view(q_out, "q_out", dev, n, heads, dim, dtype)
     _check(LIB.kv_paged_append(plan.ref, cache.ref, None if rope is None else rope.handle, kind, vq, vo, vk, vv,
                                _raw_stream(dev) if stream is None else _stream(stream, dev)))
+
+
+def kv_paged_read(plan: Plan, cache: Cache, row_start, first=None, k=None, v=None, rows=None, dtype=None,
+                  stream=None):
+    """Keys and values of every request from position first[r] on (int32 [n_req]; None: 0)
+    as rows row_start[r] .. row_start[r+1] - 1 (int32 [n_req+1]) of k and v: [rows,
+    kv_heads, dim] bfloat16 / float16.  k and v go together; where they are None they are
+    made, with `rows` rows (rows that nothing is read into hold anything) of `dtype`,
+    the cache's own or bfloat16.  Returns (k, v)."""
+    dev = _device()
+    b, _ = _fits(plan, cache, dev)
+    heads, _, dim = cache.shape
+    if (k is None) != (v is None):
+        raise ValueError("k and v go together")
+    if k is None:
+        if rows is None:
+            raise ValueError("either k and v or the number of rows has to be given")
+        like = cache.k
+        if dtype is None:
+            dtype = like.dtype if like.dtype in _HEAD_TYPES else torch.bfloat16
+        k, v = (_output(like, (int(rows), heads, dim), stream, dev, dtype) for _ in range(2))
+    elif dtype is not None and dtype is not k.dtype:
+        raise ValueError(f"k has dtype {k.dtype}; expected {dtype}")
+    n = k.shape[0] if rows is None else int(rows)
+    dtype = k.dtype
+    kind, vk, vv = _dtype(dtype, "k"), _view(k, "k", dev, n, heads, dim, dtype), _view(v, "v", dev, n, heads, dim, dtype)
+    _check(LIB.kv_paged_read(plan.ref, cache.ref, kind, _array(row_start, "row_start", dev, torch.int32, b.n_req + 1),
+                             None if first is None else _array(first, "first", dev, torch.int32, b.n_req), n, vk, vv,
+                             _raw_stream(dev) if stream is None else _stream(stream, dev)))
+    return k, v
 
 
 def kv_paged_attention(plan: Plan, cache: Cache, q, out=None, lse=None, scale=None, stream=None):

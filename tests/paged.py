@@ -59,3 +59,16 @@ def check_attention(got, lse, want, q):
         assert torch.equal(l64[rest], ref_lse[rest])
         bad = ((l64 - ref_lse).abs() > e + 2.0 ** -21 * ref_lse.abs())[fine]
         assert not bool(bad.any())
+
+
+def held_cache(n_blocks, heads, block, dim, kind, gen):
+    """k, v of 8 bits and their scales [n_blocks, heads], as a cache that was written to has
+    them: the whole range of numbers, blocks of different sizes."""
+    most = {"i8": 127.0, "fp8": 448.0}[kind]
+
+    def numbers(*shape):
+        x = (torch.randn(*shape, generator=gen) * (most / 4)).clamp(-most, most)
+        return (x.round().to(torch.int8) if kind == "i8" else x.to(torch.float8_e4m3fn)).cuda()
+
+    scales = [(torch.rand(n_blocks, heads, generator=gen) * 3 + 1) / most for _ in range(2)]
+    return numbers(n_blocks, heads, block, dim), numbers(n_blocks, heads, dim, block), scales[0].cuda(), scales[1].cuda()
