@@ -300,87 +300,160 @@ struct ReadArgs {
   const uint8_t *kc, *vc;
   int64_t k_block, v_block;  // bytes
   const float *k_scale, *v_scale;
-  uint32_t max_rows, max_blocks, n_blocks, kv_heads, dim;
+  uint32_t max_rows, max_blocks, n_blocks, kv_heads, dim_shift;
+  uint32_t each;      // wavefronts of a run's keys, and of its values
+  uint32_t tasks;     // wavefronts in all
   uint32_t by_block;  // scales by block, or by head
 };
 
-// held types of the read: 16 bits too
+// 16-bit caches: numbers are copied
 struct Same {};
 
+// 4 numbers, times their scale, in 16 bits
+template <class V, class H>
+__device__ __forceinline__ uint2 rows4(uint32_t u, float by) {
+  typedef typename Elem<V>::type E;
+  float f[4];
+  values4<H>(u, f);
+  uint16_t h[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) h[i] = __builtin_bit_cast(uint16_t, (E)(f[i] * by));
+  return make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
+}
+
+// byte (16 bits: half) i of the result's word j is byte j of word i
+__device__ __forceinline__ void turn_bytes(uint32_t* u) {
+  const uint32_t a = __builtin_amdgcn_perm(u[1], u[0], 0x05010400u), b = __builtin_amdgcn_perm(u[3], u[2], 0x05010400u);
+  const uint32_t c = __builtin_amdgcn_perm(u[1], u[0], 0x07030602u), d = __builtin_amdgcn_perm(u[3], u[2], 0x07030602u);
+  u[0] = __builtin_amdgcn_perm(b, a, 0x05040100u), u[1] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+  u[2] = __builtin_amdgcn_perm(d, c, 0x05040100u), u[3] = __builtin_amdgcn_perm(d, c, 0x07060302u);
+}
+__device__ __forceinline__ void turn_halves(uint32_t& a, uint32_t& b) {
+  const uint32_t lo = __builtin_amdgcn_perm(b, a, 0x05040100u);
+  b = __builtin_amdgcn_perm(b, a, 0x07060302u);
+  a = lo;
+}
+
+// A wavefront reads 8 KB of a run's keys, or of its values, whatever heads these are: it
+// shares nothing with others.  Keys go as they lie, 8 elements a load.  Of the values a
+// lane takes 8 elements of as many tokens as 16 bytes hold, turns them in registers
+// and writes 16 bytes of each token's row.
 template <class V, class H>
 __global__ __launch_bounds__(256) void k_read(ReadArgs a) {
   constexpr int kBytes = __is_same(H, Same) ? 2 : 1;
-  const int tid = threadIdx.x;
-  const uint32_t head = blockIdx.x % a.kv_heads;
+  constexpr int kTokens = 16 / kBytes;  // of a lane's values
+  constexpr uint32_t kTokenShift = kBytes == 1 ? 4 : 3;
+  const uint32_t lane = lane_id();
+  const uint32_t task = blockIdx.x * 4 + wave_id();
+  if (task >= a.tasks) return;
+  const uint32_t place = task / (2 * a.each);
+  uint32_t part = task - place * (2 * a.each);
   uint32_t req, run;
-  find_run(a.runs, blockIdx.x / a.kv_heads, req, run);
+  find_run(a.runs, place, req, run);
   if (req >= a.runs.n_req) return;
-  const int64_t size = 1ll << a.runs.shift;
+  const uint32_t shift = a.runs.shift;
   const int64_t t0 = a.runs.start[req], t1 = min((int64_t)a.runs.start[req + 1], (int64_t)a.max_rows);
   if (t0 < 0 || t0 >= t1) return;
   const int64_t first = a.first ? a.first[req] : 0;
-  const int64_t block0 = ((first >> a.runs.shift) + run) << a.runs.shift;
-  const int64_t from = max(first, block0), to = min(first + (t1 - t0), block0 + size);
+  const int64_t column = (first >> shift) + run, block0 = column << shift;
+  const int64_t from = max(first, block0), to = min(first + (t1 - t0), block0 + (1ll << shift));
   if (from >= to) return;
-  const uint32_t row = (uint32_t)(t0 + (from - first)), n = (uint32_t)(to - from), at = (uint32_t)(from - block0);
-  // rows that are in the cache: the block's first tokens, or none
-  const int64_t column = block0 >> a.runs.shift;
+  // Places begin .. end - 1 of the block are rows, those before `have` are in the cache.
+  const uint32_t begin = (uint32_t)(from - block0), end = (uint32_t)(to - block0);
+  const int64_t row0 = t0 + (from - first) - begin;  // row of place 0
   int page = -1;
   if (column >= 0 && column < a.max_blocks) page = a.table[(uint64_t)req * a.max_blocks + column];
-  const int64_t end = page >= 0 && page < (int)a.n_blocks ? min((int64_t)a.kv_len[req], to) : from;
-  const uint32_t have = (uint32_t)max(end - from, (int64_t)0);
-  page = have ? page : 0;
+  const bool there = page >= 0 && page < (int)a.n_blocks;
+  const uint32_t have = there ? (uint32_t)min(max((int64_t)a.kv_len[req] - block0, (int64_t)0), (int64_t)end) : 0;
+  if (!there) page = 0;
+  const bool keys = part < a.each;
+  if (!keys) part -= a.each;
+  const float* scales = keys ? a.k_scale : a.v_scale;
+  auto scale_of = [&](uint32_t head) {
+    if (kBytes == 2 || !scales) return 1.0f;
+    return scales[(a.by_block ? (int64_t)page * a.kv_heads : 0) + head];
+  };
 
-  float ks = 1.0f, vs = 1.0f;
-  if constexpr (kBytes == 1) {
-    const int64_t i = (a.by_block ? (int64_t)page * a.kv_heads : 0) + head;
-    if (a.k_scale) ks = a.k_scale[i];
-    if (a.v_scale) vs = a.v_scale[i];
-  }
-  uint16_t* k = a.k + (int64_t)row * a.kt + head * a.kh;
-  uint16_t* v = a.v + (int64_t)row * a.vt + head * a.vh;
-  const uint8_t* kc = a.kc + page * a.k_block + (((int64_t)head << a.runs.shift) + at) * a.dim * kBytes;
-  const uint8_t* vc = a.vc + page * a.v_block + ((int64_t)head * a.dim << a.runs.shift) * kBytes;
-  const uint32_t chunks = a.dim / 8;
-  for (uint32_t i = tid; i < n * chunks; i += 256) {
-    const uint32_t t = i / chunks, c = i - t * chunks;
-    uint4 u = make_uint4(0, 0, 0, 0);
-    if (t < have) {
-      if constexpr (kBytes == 2) {
-        u = *(const uint4*)(kc + ((int64_t)t * a.dim + c * 8) * 2);
-      } else {
-        const uint2 w = *(const uint2*)(kc + (int64_t)t * a.dim + c * 8);
-        float f[8];
-        values4<H>(w.x, f);
-        values4<H>(w.y, f + 4);
+  if (keys) {
+    const uint8_t* kc = a.kc + page * a.k_block;
+    constexpr int kSteps = 16 / kBytes;  // of 64 lanes by 8 elements
+    constexpr int kAhead = 8;
+    const uint32_t chunk_shift = a.dim_shift - 3;
+#pragma unroll 1
+    for (int step = 0; step < kSteps; step += kAhead) {
+      uint4 u[kAhead];
+      float by[kAhead];
+      uint32_t at[kAhead];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] *= ks;
-        u = pack<V>(f);
-      }
-    }
-    *(uint4*)(k + (int64_t)t * a.kt + c * 8) = u;
-  }
-  // values: a strip of elements through LDS
-  __shared__ uint16_t strip[256][kStrip + 8];
-  for (uint32_t d0 = 0; d0 < a.dim; d0 += kStrip) {
-    __syncthreads();
-    for (uint32_t i = tid; i < n * kStrip; i += 256) {
-      const uint32_t d = i / n, t = i - d * n;
-      uint16_t u = 0;
-      if (t < have) {
-        const uint8_t* p = vc + (((int64_t)(d0 + d) << a.runs.shift) + at + t) * kBytes;
-        if constexpr (kBytes == 2) {
-          u = *(const uint16_t*)p;
-        } else {
-          u = __builtin_bit_cast(uint16_t, (typename Elem<V>::type)(H::template value<0>(*p) * vs));
+      for (int i = 0; i < kAhead; ++i) {
+        at[i] = (part * kSteps + step + i) * 64 + lane;
+        const uint32_t t = (at[i] >> chunk_shift) & ((1u << shift) - 1), head = at[i] >> (chunk_shift + shift);
+        u[i] = make_uint4(0, 0, 0, 0);
+        by[i] = 1.0f;
+        if (head < a.kv_heads && t >= begin && t < have) {
+          const uint8_t* p = kc + (int64_t)at[i] * 8 * kBytes;
+          if constexpr (kBytes == 2) {
+            u[i] = *(const uint4*)p;
+          } else {
+            const uint2 w = *(const uint2*)p;
+            u[i].x = w.x, u[i].y = w.y;
+            by[i] = scale_of(head);
+          }
         }
       }
-      strip[t][d] = u;
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const uint32_t t = (at[i] >> chunk_shift) & ((1u << shift) - 1), head = at[i] >> (chunk_shift + shift);
+        if (head >= a.kv_heads || t < begin || t >= end) continue;
+        if constexpr (kBytes == 1) {
+          const uint2 lo = rows4<V, H>(u[i].x, by[i]), hi = rows4<V, H>(u[i].y, by[i]);
+          u[i] = make_uint4(lo.x, lo.y, hi.x, hi.y);
+        }
+        *(uint4*)(a.k + (row0 + t) * a.kt + head * a.kh + (at[i] & ((1u << chunk_shift) - 1)) * 8) = u[i];
+      }
     }
-    __syncthreads();
-    for (uint32_t i = tid; i < n * (kStrip / 8); i += 256) {
-      const uint32_t t = i / (kStrip / 8), c = i % (kStrip / 8);
-      *(uint4*)(v + (int64_t)t * a.vt + d0 + c * 8) = *(const uint4*)&strip[t][c * 8];
+    return;
+  }
+
+  // values: item = (head, tokens, 8 elements), the elements first
+  const uint32_t item = part * 64 + lane, chunk_shift = a.dim_shift - 3;
+  const uint32_t d = (item & ((1u << chunk_shift) - 1)) * 8;
+  const uint32_t t = (item >> chunk_shift << kTokenShift) & ((1u << shift) - 1);
+  const uint32_t head = item >> (chunk_shift + shift - kTokenShift);
+  if (head >= a.kv_heads || t + kTokens <= begin || t >= end) return;
+  uint4 u[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) u[i] = make_uint4(0, 0, 0, 0);
+  float by = 1.0f;
+  if (t < have) {
+    by = scale_of(head);
+    const uint8_t* p = a.vc + page * a.v_block + (((((int64_t)head << a.dim_shift) + d) << shift) + t) * kBytes;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) u[i] = *(const uint4*)(p + ((int64_t)(i * kBytes) << shift));
+  }
+  uint16_t* out = a.v + (row0 + t) * a.vt + head * a.vh + d;
+  auto put = [&](int i, const uint4& w) {
+    const uint32_t at = t + i;
+    if (at >= begin && at < end) *(uint4*)(out + i * a.vt) = at < have ? w : make_uint4(0, 0, 0, 0);
+  };
+  auto word = [](const uint4& w, int i) { return i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w; };
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {  // a word of 4 tokens, or of 2
+    uint32_t lo[4], hi[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) lo[i] = word(u[i], w), hi[i] = word(u[4 + i], w);
+    if constexpr (kBytes == 1) {
+      turn_bytes(lo);
+      turn_bytes(hi);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint2 x = rows4<V, H>(lo[i], by), y = rows4<V, H>(hi[i], by);
+        put(4 * w + i, make_uint4(x.x, x.y, y.x, y.y));
+      }
+    } else {
+      turn_halves(lo[0], lo[1]), turn_halves(lo[2], lo[3]), turn_halves(hi[0], hi[1]), turn_halves(hi[2], hi[3]);
+      put(2 * w, make_uint4(lo[0], lo[2], hi[0], hi[2]));
+      put(2 * w + 1, make_uint4(lo[1], lo[3], hi[1], hi[3]));
     }
   }
 }
@@ -455,13 +528,16 @@ kv_status paged_read(const kv_paged_batch& b, const kv_paged_cache& c, uint32_t 
   a.k_scale = c.k_scale, a.v_scale = c.v_scale;
   a.by_block = by_block(c.dtype);
   a.max_rows = max_rows, a.max_blocks = b.max_blocks, a.n_blocks = c.n_blocks;
-  a.kv_heads = b.kv_heads, a.dim = b.head_dim;
-  const uint64_t grid = plan_runs(a.runs, row_start, b.n_req, b.block_size, max_rows, max_rows) * b.kv_heads;
-  if (grid > 0x7fffffffull) return fail(KV_ERR_UNSUPPORTED, "kv_paged_read: too many rows for one call");
+  a.kv_heads = b.kv_heads, a.dim_shift = (uint32_t)__builtin_ctz(b.head_dim);
+  a.each = (uint32_t)(((uint64_t)b.kv_heads * b.block_size * b.head_dim * bytes + 8191) / 8192);
+  const uint64_t tasks = plan_runs(a.runs, row_start, b.n_req, b.block_size, max_rows, max_rows) * 2 * a.each;
+  if (tasks > 0x7fffffffull) return fail(KV_ERR_UNSUPPORTED, "kv_paged_read: too many rows for one call");
+  a.tasks = (uint32_t)tasks;
+  const uint32_t grid = (uint32_t)((tasks + 3) / 4);
   if (dtype == KV_DT_BF16)
-    launch_read<bf16x8>(a, c.dtype, (uint32_t)grid, s);
+    launch_read<bf16x8>(a, c.dtype, grid, s);
   else
-    launch_read<f16x8>(a, c.dtype, (uint32_t)grid, s);
+    launch_read<f16x8>(a, c.dtype, grid, s);
   KV_HIP(hipGetLastError());
   return KV_OK;
 }
