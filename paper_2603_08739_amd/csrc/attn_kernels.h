@@ -261,11 +261,13 @@ constexpr float kSlack = 8.0f;
 constexpr float kWeights = 16384.0f;
 
 template <class T, int D, Kind kKind>
-__global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 4) void k_attn_tile(AttnArgs a) {
+__global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : kKind == kI8Block ? 3 : 4) void k_attn_tile(AttnArgs a) {
   constexpr bool k8 = kKind != kSixteen, kByBlock = kKind >= kFp8Block;
   constexpr bool kFinite = kKind == kI8Block;  // nothing held is anything else
+  constexpr bool kStage = kKind == kI8Block && D <= 128;  // widened on the way into LDS
+  constexpr bool kNarrow = k8 && !kStage;                 // 8 bits in LDS
   constexpr int BK = 64, kBytes = k8 ? 1 : 2;
-  typedef TileLds<D, kBytes> L;
+  typedef TileLds<D, kNarrow ? 1 : 2> L;
   __shared__ uint4 k_lds0[L::kChunks], k_lds1[L::kChunks], v_lds0[L::kChunks], v_lds1[L::kChunks];
   __shared__ int mend;
   __shared__ float2 scales[kByBlock ? 4 : 1][kByBlock ? 4 : 1];
@@ -291,7 +293,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 4) void k_attn_t
     const uint16_t* p = a.q + (int64_t)(it.q_start + token) * a.qt + (int64_t)(head * G + gh) * a.qh;
 #pragma unroll
     for (int s = 0; s < D / 16; ++s)
-      qf[s] = *(const uint4*)(p + (k8 ? 32 * (s / 2) + 16 * half + 8 * (s % 2) : 16 * s + 8 * half));
+      qf[s] = *(const uint4*)(p + (kNarrow ? 32 * (s / 2) + 16 * half + 8 * (s % 2) : 16 * s + 8 * half));
   }
   // positions of the wave's first and last queries
   const int first_pos = it.ctx + (it.row0 + 32 * wave) / (int)G;
@@ -310,10 +312,16 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 4) void k_attn_t
   const uint8_t* k_base = a.k + ((int64_t)head * D * kBytes << a.shift);
   const uint8_t* v_base = a.v + ((int64_t)head * D * kBytes << a.shift);
   // this lane's places in a group of 16 keys
-  uint32_t k_from[L::kLoads], v_from[L::kLoads];
+  constexpr int kLoads = kStage ? L::kLoads / 2 : L::kLoads;
+  uint32_t k_from[kLoads], v_from[kLoads];
 #pragma unroll
-  for (int i = 0; i < L::kLoads; ++i) {
+  for (int i = 0; i < kLoads; ++i) {
     const int x = 64 * i + lane;  // chunk of the group
+    if constexpr (kStage) {
+      k_from[i] = (uint32_t)x * 16;
+      v_from[i] = (uint32_t)x << a.shift;
+      continue;
+    }
     const int r = x / L::kRowChunks;
     k_from[i] = (uint32_t)(r * L::kRowChunks + ((x % L::kRowChunks) ^ L::k_swap(16 * wave + r))) * 16;
     const int d = kBytes == 2 ? x / 2 : x;
@@ -324,23 +332,42 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 4) void k_attn_t
   // block 0.
   auto there = [&](int page) { return page >= 0 && page < (int)a.n_blocks; };
   auto look_up = [&](int key) { return table[min(key + 16 * (lane & 3), it.key_end - 1) >> a.shift]; };
+  [[maybe_unused]] uint4 k_here[kStage ? kLoads : 1], v_here[kStage ? kLoads : 1];
   auto fetch = [&](int key, int pages, uint4* lk, uint4* lv) {
     const int k16 = min(key + 16 * wave, (it.key_end - 1) & ~15);
     int page = __builtin_amdgcn_readlane(pages, wave);
     if (!there(page)) page = 0;
     const uint8_t* kp = k_base + page * a.k_block * kBytes + (int64_t)(k16 & bs_mask) * D * kBytes;
     const uint8_t* vp = v_base + page * a.v_block * kBytes + (k16 & bs_mask) * kBytes;
+    if constexpr (kStage) {
 #pragma unroll
-    for (int i = 0; i < L::kLoads; ++i) load_to_lds(kp + k_from[i], lk + (wave * L::kLoads + i) * 64);
+      for (int i = 0; i < kLoads; ++i) k_here[i] = *(const uint4*)(kp + k_from[i]), v_here[i] = *(const uint4*)(vp + v_from[i]);
+      return;
+    }
 #pragma unroll
-    for (int i = 0; i < L::kLoads; ++i) load_to_lds(vp + v_from[i], lv + (wave * L::kLoads + i) * 64);
+    for (int i = 0; i < kLoads; ++i) load_to_lds(kp + k_from[i], lk + (wave * kLoads + i) * 64);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load_to_lds(vp + v_from[i], lv + (wave * kLoads + i) * 64);
+  };
+  // Whole numbers take three instructions for two to widen, and every wavefront reads all of the
+  // tile: they are widened once, by the one that has loaded them.
+  [[maybe_unused]] auto put = [&](uint4* lk, uint4* lv) {
+    constexpr int kRow = D / 16;  // chunks of 16 numbers of a key
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int x = 64 * i + lane, r = 16 * wave + x / kRow, ch = 2 * (x % kRow);
+      lk[L::k_at(r, ch)] = widen8<T, kKind>(k_here[i].x, k_here[i].y);
+      lk[L::k_at(r, ch + 1)] = widen8<T, kKind>(k_here[i].z, k_here[i].w);
+      lv[L::v_at(wave, x, 0)] = widen8<T, kKind>(v_here[i].x, v_here[i].y);
+      lv[L::v_at(wave, x, 1)] = widen8<T, kKind>(v_here[i].z, v_here[i].w);
+    }
   };
 
   // The lane's results e = 0..15 of the first product's block n are keys 32*n + 16*(e/8)
   // + 8*half + e%8 (8 bits: 32*n + 16*half + e); the row of K that gives them:
-  const int krow = k8 ? ((col & 4) << 2) | ((col & 24) >> 1) | (col & 3) : (col & 19) | ((col & 4) << 1) | ((col & 8) >> 1);
+  const int krow = kNarrow ? ((col & 4) << 2) | ((col & 24) >> 1) | (col & 3) : (col & 19) | ((col & 4) << 1) | ((col & 8) >> 1);
   auto v_frag = [&](const uint4* lv, int i, int kb) {
-    if (k8) {
+    if (kNarrow) {
       const uint4 u = lv[L::v_at((kb & ~1) + half, 32 * i + col, 0)];
       return kb & 1 ? widen8<T, kKind>(u.z, u.w) : widen8<T, kKind>(u.x, u.y);
     }
@@ -409,20 +436,22 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 4) void k_attn_t
     if (lane < 4) scales[kByBlock ? wave : 0][kByBlock ? lane : 0] = make_float2(score_factor(c, k_next), __builtin_amdgcn_logf(in_units(v, unit)));
   };
 
-  // of the group that holds this lane's keys of block n
-  [[maybe_unused]] auto mine = [&](int n) {
-    int at = half;
+  // of the group that holds this lane's keys 8h .. 8h + 7 of block n
+  [[maybe_unused]] auto mine = [&](int n, int h) {
+    int at = kNarrow ? half : h;
     asm volatile("" : "+v"(at));  // read where it is used, each time
     return scales[kByBlock ? wave : 0][kByBlock ? 2 * n + at : 0];
   };
 
   int pages = look_up(it.key_begin), next_pages = look_up(it.key_begin + BK);
   uint32_t valid = 0;  // groups of 16 keys that are there
-  auto arrive = [&](int key, uint4* lv, uint4* next_k, uint4* next_v) __attribute__((always_inline)) {
+  auto arrive = [&](int key, uint4* lk, uint4* lv, uint4* next_k, uint4* next_v) __attribute__((always_inline)) {
     valid = (uint32_t)__ballot(there(pages) && key + 16 * (lane & 3) < it.key_end) & 15u;
     // This wavefront's loads to LDS have arrived.  They are counted with the loads
     // from memory, which the barrier itself does not wait for.
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if constexpr (!kStage) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if constexpr (kStage)
+      if (key < it.key_end) put(lk, lv);
     if constexpr (!kFinite)
       if (key < it.key_end) clean(key, valid, lv);
     if constexpr (kByBlock) take_scales(key, pages);
@@ -453,7 +482,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 4) void k_attn_t
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
         s[n] = f32x16{};
-        if (k8) {
+        if (kNarrow) {
 #pragma unroll
           for (int d = 0; d < D / 32; ++d) {
             const uint4 u = lk[L::k_at(32 * n + krow, 2 * d + half)];
@@ -466,26 +495,30 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 4) void k_attn_t
         }
       }
       if (edge) {
-        constexpr int kRun = k8 ? 16 : 8;
+        constexpr int kRun = kNarrow ? 16 : 8;
         const int from = key + kRun * half, most = qpos - from, least = qpos - window - from;
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const int at = 32 * n + (k8 ? e : 16 * (e >> 3) + (e & 7));  // + kRun * half: the key
-            const bool here = (valid >> (2 * n + (k8 ? half : e >> 3))) & 1;
+            const int at = 32 * n + (kNarrow ? e : 16 * (e >> 3) + (e & 7));  // + kRun * half: the key
+            const bool here = (valid >> (2 * n + (kNarrow ? half : e >> 3))) & 1;
             s[n][e] = (here & (at <= most) & (at > least)) ? s[n][e] : -__builtin_inff();
           }
       }
       if (look) {
         float top = s[0][0];
         if constexpr (kByBlock) {
-          float most[2] = {s[0][0], s[1][0]};
+          top = -__builtin_inff();
 #pragma unroll
           for (int n = 0; n < 2; ++n)
 #pragma unroll
-            for (int e = 0; e < 16; e += 2) most[n] = max3(most[n], s[n][e], s[n][e + 1]);
-          top = max2(most[0] * mine(0).x, most[1] * mine(1).x);
+            for (int h = 0; h < (kNarrow ? 1 : 2); ++h) {
+              float most = s[n][8 * h];
+#pragma unroll
+              for (int e = 0; e < (kNarrow ? 16 : 8); e += 2) most = max3(most, s[n][8 * h + e], s[n][8 * h + e + 1]);
+              top = max2(top, most * mine(n, h).x);
+            }
           top = max2(top, other_half(top)) - T::kLift;
         } else {
 #pragma unroll
@@ -510,11 +543,18 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 4) void k_attn_t
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
         float from = -sub, by = c;
-        if constexpr (kByBlock) from = mine(n).y - sub, by = mine(n).x;
+        if constexpr (kByBlock) {
+          const float2 f = mine(n, 0);
+          from = f.y - sub, by = f.x;
+        }
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
+          if (kByBlock && !kNarrow && e == 8) {
+            const float2 f = mine(n, 1);
+            from = f.y - sub, by = f.x;
+          }
           s[n][e] = __builtin_amdgcn_exp2f(fmaf(s[n][e], by, from));
-          sum[kByBlock ? 2 * n + (e & 1) : e & 3] += s[n][e];
+          sum[!kByBlock ? e & 3 : kNarrow ? 2 * n + (e & 1) : 2 * n + (e >> 3)] += s[n][e];
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -522,9 +562,13 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 4) void k_attn_t
                                     T::pack(s[n][8 * h + 4], s[n][8 * h + 5]), T::pack(s[n][8 * h + 6], s[n][8 * h + 7]));
       }
       float all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-      if constexpr (kByBlock) {
-        all = (sum[0] + sum[1]) * __builtin_amdgcn_exp2f(-mine(0).y);
-        all = fmaf(sum[2] + sum[3], __builtin_amdgcn_exp2f(-mine(1).y), all);
+      if constexpr (kByBlock && kNarrow) {
+        all = (sum[0] + sum[1]) * __builtin_amdgcn_exp2f(-mine(0, 0).y);
+        all = fmaf(sum[2] + sum[3], __builtin_amdgcn_exp2f(-mine(1, 0).y), all);
+      } else if constexpr (kByBlock) {
+        all = sum[0] * __builtin_amdgcn_exp2f(-mine(0, 0).y);
+#pragma unroll
+        for (int x = 1; x < 4; ++x) all = fmaf(sum[x], __builtin_amdgcn_exp2f(-mine(x >> 1, x & 1).y), all);
       }
       if (!kLazy || look || !__any(!(all <= kWeights))) {
         l += all;
@@ -549,9 +593,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : 4) void k_attn_t
   // two tiles a turn: their places in LDS are known to the compiler, which waits for
   // loads to LDS before any read that they might concern
   for (int key = it.key_begin; key < it.key_end; key += 2 * BK) {
-    arrive(key, v_lds0, k_lds1, v_lds1);
+    arrive(key, k_lds0, v_lds0, k_lds1, v_lds1);
     if (active(key)) multiply(key, k_lds0, v_lds0);
-    arrive(key + BK, v_lds1, k_lds0, v_lds0);
+    arrive(key + BK, k_lds1, v_lds1, k_lds0, v_lds0);
     if (active(key + BK)) multiply(key + BK, k_lds1, v_lds1);
   }
   // What was taken out, added to what has been stored for this lane's query (an
