@@ -121,6 +121,18 @@ __device__ __forceinline__ uint4 widen8(uint32_t a, uint32_t b) {
                       T::template widen<true>(b));
 }
 
+// The type of weights and values in the second product: the queries', but for whole
+// numbers float16 whatever that is, which takes fewer instructions to widen them to (8
+// significant bits are exact in both) and rounds weights less.
+template <class T, Kind kKind>
+struct Weights {
+  typedef T type;
+};
+template <class T>
+struct Weights<T, kI8Block> {
+  typedef F16 type;
+};
+
 struct AttnArgs {
   const uint16_t* q;
   uint16_t* out;
@@ -261,16 +273,17 @@ constexpr float kSlack = 8.0f;
 constexpr float kWeights = 16384.0f;
 
 template <class T, int D, Kind kKind>
-__global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : kKind == kI8Block ? 3 : 4) void k_attn_tile(AttnArgs a) {
+__global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : kKind >= kFp8Block ? 3 : 4) void k_attn_tile(AttnArgs a) {
   constexpr bool k8 = kKind != kSixteen, kByBlock = kKind >= kFp8Block;
   constexpr bool kFinite = kKind == kI8Block;  // nothing held is anything else
+  typedef typename Weights<T, kKind>::type P;
   constexpr bool kStage = kKind == kI8Block && D <= 128;  // widened on the way into LDS
   constexpr bool kNarrow = k8 && !kStage;                 // 8 bits in LDS
   constexpr int BK = 64, kBytes = k8 ? 1 : 2;
   typedef TileLds<D, kNarrow ? 1 : 2> L;
   __shared__ uint4 k_lds0[L::kChunks], k_lds1[L::kChunks], v_lds0[L::kChunks], v_lds1[L::kChunks];
   __shared__ int mend;
-  __shared__ float2 scales[kByBlock ? 4 : 1][kByBlock ? 4 : 1];
+  __shared__ float scales[kByBlock ? 2 : 1][kByBlock ? 4 : 1][kByBlock ? 4 : 1][4];
   const uint32_t item = blockIdx.x / a.kv_heads, head = blockIdx.x % a.kv_heads;
   const PieceItem it = a.items[item];  // loaded whether there is one or not: one wait for both
   if ((int)item >= a.head->n_items || a.head->sizes != a.sizes) return;
@@ -349,8 +362,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : kKind == kI8Bloc
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) load_to_lds(vp + v_from[i], lv + (wave * kLoads + i) * 64);
   };
-  // Whole numbers take three instructions for two to widen, and every wavefront reads all of the
-  // tile: they are widened once, by the one that has loaded them.
+  // Whole numbers take two or three instructions for two to widen, and every wavefront reads all
+  // of the tile: they are widened once, by the one that has loaded them.  (With loads of 8 bytes
+  // its writes to LDS would not meet on banks, but the prompt takes 860 us for 830.)
   [[maybe_unused]] auto put = [&](uint4* lk, uint4* lv) {
     constexpr int kRow = D / 16;  // chunks of 16 numbers of a key
 #pragma unroll
@@ -358,8 +372,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : kKind == kI8Bloc
       const int x = 64 * i + lane, r = 16 * wave + x / kRow, ch = 2 * (x % kRow);
       lk[L::k_at(r, ch)] = widen8<T, kKind>(k_here[i].x, k_here[i].y);
       lk[L::k_at(r, ch + 1)] = widen8<T, kKind>(k_here[i].z, k_here[i].w);
-      lv[L::v_at(wave, x, 0)] = widen8<T, kKind>(v_here[i].x, v_here[i].y);
-      lv[L::v_at(wave, x, 1)] = widen8<T, kKind>(v_here[i].z, v_here[i].w);
+      lv[L::v_at(wave, x, 0)] = widen8<P, kKind>(v_here[i].x, v_here[i].y);
+      lv[L::v_at(wave, x, 1)] = widen8<P, kKind>(v_here[i].z, v_here[i].w);
     }
   };
 
@@ -369,7 +383,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : kKind == kI8Bloc
   auto v_frag = [&](const uint4* lv, int i, int kb) {
     if (kNarrow) {
       const uint4 u = lv[L::v_at((kb & ~1) + half, 32 * i + col, 0)];
-      return kb & 1 ? widen8<T, kKind>(u.z, u.w) : widen8<T, kKind>(u.x, u.y);
+      return kb & 1 ? widen8<P, kKind>(u.z, u.w) : widen8<P, kKind>(u.x, u.y);
     }
     return lv[L::v_at(kb, 32 * i + col, half)];
   };
@@ -411,62 +425,62 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : kKind == kI8Bloc
   // multiplied by the values' on their way into the second product, relative to a power of
   // two that follows the largest seen (o counts in units of it), so that they stay in the range of
   // 16 bits; in the exponent again, where it costs nothing, and the sum of weights undoes it.
-  // Lane i loads the scales of group i % 4, one tile ahead; a group that no row of the tile
-  // sees has none.  What comes of them, factor and logarithm, goes through LDS, a place for
-  // each wavefront: kept in registers over the products, they would be too many.
+  // Lane i loads the scales of group i % 4 two tiles ahead; a group that no row of the tile
+  // sees has none.  What comes of them goes through LDS a tile ahead, in a place for each
+  // wavefront: kept in registers over the products, they would be too many.
   [[maybe_unused]] float k_next = 0.0f, v_next = 0.0f;
-  [[maybe_unused]] uint32_t unit = 0;  // the power's exponent bits
+  [[maybe_unused]] uint32_t unit = 0, unit_now = 0, unit_here = 0;  // the power's exponent bits: of the tile to come, of the present one, of o
   [[maybe_unused]] auto load_scales = [&](int page) {
     const int64_t from = (int64_t)(there(page) ? page : 0) * a.kv_heads + head;
     k_next = a.k_scale[from], v_next = a.v_scale[from];
   };
-  [[maybe_unused]] auto take_scales = [&](int key, int page) {
+  [[maybe_unused]] auto take_scales = [&](int key, int page, int turn) {
     const int k16 = key + 16 * (lane & 3);
     const bool seen = there(page) && k16 < it.key_end && k16 <= tile_last && k16 + 15 > tile_first - window;
     const float v = seen ? v_next : 0.0f;
-    const uint32_t e = (uint32_t)__builtin_amdgcn_readfirstlane((int)(most_of_four(__builtin_bit_cast(uint32_t, v) & 0x7fffffffu) >> 23));
-    if (e > unit) {
-      const float less = unit_ratio(unit, e);
-      unit = e;
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-        for (int x = 0; x < 16; ++x) o[i][x] *= less;
-    }
-    if (lane < 4) scales[kByBlock ? wave : 0][kByBlock ? lane : 0] = make_float2(score_factor(c, k_next), __builtin_amdgcn_logf(in_units(v, unit)));
+    unit = max(unit, (uint32_t)__builtin_amdgcn_readfirstlane((int)(most_of_four(__builtin_bit_cast(uint32_t, v) & 0x7fffffffu) >> 23)));
+    const float l2 = __builtin_amdgcn_logf(in_units(v, unit));
+    if (lane < 4) *(float4*)scales[kByBlock ? turn : 0][kByBlock ? wave : 0][kByBlock ? lane : 0] = make_float4(score_factor(c, k_next), l2, __builtin_amdgcn_exp2f(-l2), 0.0f);
   };
-
-  // of the group that holds this lane's keys 8h .. 8h + 7 of block n
-  [[maybe_unused]] auto mine = [&](int n, int h) {
-    int at = kNarrow ? half : h;
-    asm volatile("" : "+v"(at));  // read where it is used, each time
-    return scales[kByBlock ? wave : 0][kByBlock ? 2 * n + at : 0];
-  };
-
   int pages = look_up(it.key_begin), next_pages = look_up(it.key_begin + BK);
+  [[maybe_unused]] int third_pages = 0;
   uint32_t valid = 0;  // groups of 16 keys that are there
-  auto arrive = [&](int key, uint4* lk, uint4* lv, uint4* next_k, uint4* next_v) __attribute__((always_inline)) {
+  auto arrive = [&](int key, [[maybe_unused]] int turn, uint4* lv, uint4* next_k, uint4* next_v) __attribute__((always_inline)) {
     valid = (uint32_t)__ballot(there(pages) && key + 16 * (lane & 3) < it.key_end) & 15u;
     // This wavefront's loads to LDS have arrived.  They are counted with the loads
     // from memory, which the barrier itself does not wait for.
     if constexpr (!kStage) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    if constexpr (kStage)
-      if (key < it.key_end) put(lk, lv);
     if constexpr (!kFinite)
       if (key < it.key_end) clean(key, valid, lv);
-    if constexpr (kByBlock) take_scales(key, pages);
     __syncthreads();  // everybody's have, and nobody reads the other keys any more
-    if (key + BK < it.key_end) {
-      fetch(key + BK, next_pages, next_k, next_v);
-      if constexpr (kByBlock) load_scales(next_pages);
+    if constexpr (kByBlock) {
+      unit_now = unit;
+      take_scales(key + BK, next_pages, turn ^ 1);
     }
-    pages = next_pages;
-    next_pages = look_up(key + 2 * BK);
+    if constexpr (!kStage)
+      if (key + BK < it.key_end) fetch(key + BK, next_pages, next_k, next_v);
+    if constexpr (kByBlock) {
+      load_scales(third_pages);
+      pages = next_pages;
+      next_pages = third_pages;
+      third_pages = look_up(key + 3 * BK);
+    } else {
+      pages = next_pages;
+      next_pages = look_up(key + 2 * BK);
+    }
+  };
+  // Numbers that are widened are loaded two tiles ahead.  They go into LDS while the present
+  // tile's second products run.  (`pages` and `next_pages` are those of the next tiles by then.)
+  [[maybe_unused]] auto stage = [&](int key, uint4* next_k, uint4* next_v) __attribute__((always_inline)) {
+    // (also past the end, where the last keys are read again: with loads that may or may not
+    // have been sent, the compiler waits for all of them where it needs an earlier one)
+    put(next_k, next_v);
+    fetch(key + 2 * BK, next_pages, nullptr, nullptr);
   };
   auto active = [&](int key) {
     return wave_on && key < it.key_end && key <= last_pos && key + BK > first_pos - window + 1;
   };
-  auto multiply = [&](int key, const uint4* lk, const uint4* lv) __attribute__((always_inline)) {
+  auto multiply = [&](int key, [[maybe_unused]] int turn, const uint4* lk, const uint4* lv) __attribute__((always_inline)) {
     const bool edge = key + BK - 1 > first_pos || key <= last_pos - window || valid != 15;
     // Weights are taken from the maximum of the keys seen when it was last looked for
     // (at first, and again when a weight has grown past kWeights: their sum, at
@@ -477,6 +491,28 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : kKind == kI8Bloc
     constexpr bool kLazy = D <= 128;
     f32x16 s[2];
     uint4 p[4];
+    if constexpr (kByBlock)
+      if (unit_here != unit_now) {
+        const float less = unit_ratio(unit_here, unit_now);
+        unit_here = unit_now;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+          for (int x = 0; x < 16; ++x) o[i][x] *= less;
+      }
+    // Of the groups that hold this lane's keys 8h .. 8h + 7 of blocks n: factor, logarithm and
+    // what undoes it.
+    constexpr int kGroups = kNarrow ? 1 : 2;  // of a block n
+    [[maybe_unused]] float factor[2][kGroups], log2v[2][kGroups], undo[2][kGroups];
+    if constexpr (kByBlock) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int h = 0; h < kGroups; ++h) {
+          const float4 f = *(const float4*)scales[turn][wave][2 * n + (kNarrow ? half : h)];
+          factor[n][h] = f.x, log2v[n][h] = f.y, undo[n][h] = f.z;
+        }
+    }
     bool look = !kLazy || __any(m == -__builtin_inff());
     for (;;) {
 #pragma unroll
@@ -496,7 +532,10 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : kKind == kI8Bloc
       }
       if (edge) {
         constexpr int kRun = kNarrow ? 16 : 8;
-        const int from = key + kRun * half, most = qpos - from, least = qpos - window - from;
+        const int from = key + kRun * half;
+        int most = qpos - from, least = qpos - window - from;
+        // (worked out ahead of this loop, the masks would take more scalar registers than there are)
+        if constexpr (kByBlock) asm volatile("" : "+v"(most), "+v"(least));
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
@@ -513,19 +552,19 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : kKind == kI8Bloc
 #pragma unroll
           for (int n = 0; n < 2; ++n)
 #pragma unroll
-            for (int h = 0; h < (kNarrow ? 1 : 2); ++h) {
+            for (int h = 0; h < kGroups; ++h) {
               float most = s[n][8 * h];
 #pragma unroll
               for (int e = 0; e < (kNarrow ? 16 : 8); e += 2) most = max3(most, s[n][8 * h + e], s[n][8 * h + e + 1]);
-              top = max2(top, most * mine(n, h).x);
+              top = max2(top, most * factor[n][h]);
             }
-          top = max2(top, other_half(top)) - T::kLift;
+          top = max2(top, other_half(top)) - P::kLift;
         } else {
 #pragma unroll
           for (int n = 0; n < 2; ++n)
 #pragma unroll
             for (int e = 0; e < 16; e += 2) top = max3(top, s[n][e], s[n][e + 1]);
-          top = fmaf(max2(top, other_half(top)), c, -T::kLift);
+          top = fmaf(max2(top, other_half(top)), c, -P::kLift);
         }
         if (kLazy || __any(top > m + kSlack)) {
           const float m_new = fmaxf(m, top);
@@ -543,32 +582,26 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : kKind == kI8Bloc
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
         float from = -sub, by = c;
-        if constexpr (kByBlock) {
-          const float2 f = mine(n, 0);
-          from = f.y - sub, by = f.x;
-        }
+        if constexpr (kByBlock) from = log2v[n][0] - sub, by = factor[n][0];
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          if (kByBlock && !kNarrow && e == 8) {
-            const float2 f = mine(n, 1);
-            from = f.y - sub, by = f.x;
-          }
+          if constexpr (kByBlock && !kNarrow)
+            if (e == 8) from = log2v[n][1] - sub, by = factor[n][1];
           s[n][e] = __builtin_amdgcn_exp2f(fmaf(s[n][e], by, from));
           sum[!kByBlock ? e & 3 : kNarrow ? 2 * n + (e & 1) : 2 * n + (e >> 3)] += s[n][e];
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-          p[2 * n + h] = make_uint4(T::pack(s[n][8 * h], s[n][8 * h + 1]), T::pack(s[n][8 * h + 2], s[n][8 * h + 3]),
-                                    T::pack(s[n][8 * h + 4], s[n][8 * h + 5]), T::pack(s[n][8 * h + 6], s[n][8 * h + 7]));
+          p[2 * n + h] = make_uint4(P::pack(s[n][8 * h], s[n][8 * h + 1]), P::pack(s[n][8 * h + 2], s[n][8 * h + 3]),
+                                    P::pack(s[n][8 * h + 4], s[n][8 * h + 5]), P::pack(s[n][8 * h + 6], s[n][8 * h + 7]));
       }
       float all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
       if constexpr (kByBlock && kNarrow) {
-        all = (sum[0] + sum[1]) * __builtin_amdgcn_exp2f(-mine(0, 0).y);
-        all = fmaf(sum[2] + sum[3], __builtin_amdgcn_exp2f(-mine(1, 0).y), all);
+        all = fmaf(sum[2] + sum[3], undo[1][0], (sum[0] + sum[1]) * undo[0][0]);
       } else if constexpr (kByBlock) {
-        all = sum[0] * __builtin_amdgcn_exp2f(-mine(0, 0).y);
+        all = sum[0] * undo[0][0];
 #pragma unroll
-        for (int x = 1; x < 4; ++x) all = fmaf(sum[x], __builtin_amdgcn_exp2f(-mine(x >> 1, x & 1).y), all);
+        for (int x = 1; x < 4; ++x) all = fmaf(sum[x], undo[x >> 1][x & 1], all);
       }
       if (!kLazy || look || !__any(!(all <= kWeights))) {
         l += all;
@@ -583,20 +616,30 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : kKind == kI8Bloc
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
-      for (int kb = 0; kb < 4; ++kb) o[i] = T::mfma32(v_frag(lv, i, kb), p[kb], o[i]);
+      for (int kb = 0; kb < 4; ++kb) o[i] = P::mfma32(v_frag(lv, i, kb), p[kb], o[i]);
   };
 
   if (tid == 0) mend = 0;
   fetch(it.key_begin, pages, k_lds0, v_lds0);
-  if constexpr (kByBlock) load_scales(pages);
+  if constexpr (kByBlock) {
+    load_scales(pages);
+    if constexpr (kStage) put(k_lds0, v_lds0);
+    take_scales(it.key_begin, pages, 0);
+    // in the order in which the loop sends them: it waits for some of them only
+    load_scales(next_pages);
+    third_pages = look_up(it.key_begin + 2 * BK);
+    if constexpr (kStage) fetch(it.key_begin + BK, next_pages, nullptr, nullptr);
+  }
   __syncthreads();  // mend
   // two tiles a turn: their places in LDS are known to the compiler, which waits for
   // loads to LDS before any read that they might concern
   for (int key = it.key_begin; key < it.key_end; key += 2 * BK) {
-    arrive(key, k_lds0, v_lds0, k_lds1, v_lds1);
-    if (active(key)) multiply(key, k_lds0, v_lds0);
-    arrive(key + BK, k_lds1, v_lds1, k_lds0, v_lds0);
-    if (active(key + BK)) multiply(key + BK, k_lds1, v_lds1);
+    arrive(key, 0, v_lds0, k_lds1, v_lds1);
+    if constexpr (kStage) stage(key, k_lds1, v_lds1);
+    if (active(key)) multiply(key, 0, k_lds0, v_lds0);
+    arrive(key + BK, 1, v_lds1, k_lds0, v_lds0);
+    if constexpr (kStage) stage(key + BK, k_lds0, v_lds0);
+    if (active(key + BK)) multiply(key + BK, 1, k_lds1, v_lds1);
   }
   // What was taken out, added to what has been stored for this lane's query (an
   // infinity or a NaN decides its element whatever the scale).
@@ -619,7 +662,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : kKind == kI8Bloc
   const bool mended = !kFinite && mend != 0;
   l += other_half(l);
   if constexpr (kByBlock) {
-    const float one = unit_value(unit);
+    const float one = unit_value(unit_here);
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
@@ -677,6 +720,7 @@ template <class T, int D, Kind kKind, int NC>
 __global__ __launch_bounds__(256, D * NC <= 128 ? 2 : 1) void k_attn_rows(AttnArgs a) {
   constexpr bool k8 = kKind != kSixteen, kByBlock = kKind >= kFp8Block;
   constexpr bool kFinite = kKind == kI8Block;  // nothing held is anything else
+  typedef typename Weights<T, kKind>::type P;
   constexpr int kPer = k8 ? 16 : 8, kKeys = 4 * kPer, kBlocks = kKeys / 16, kSteps = kKeys / 32;
   constexpr int kLoadsK = D / 4 / kPer;  // 16-byte loads of a key row by a lane
   const uint32_t item = blockIdx.x / a.kv_heads, head = blockIdx.x % a.kv_heads;
@@ -843,7 +887,7 @@ __global__ __launch_bounds__(256, D * NC <= 128 ? 2 : 1) void k_attn_rows(AttnAr
       }
       if constexpr (kByBlock) top *= cv;
       top = max2(top, __shfl_xor(top, 16, 64));
-      top = kByBlock ? max2(top, other_half(top)) - T::kLift : fmaf(max2(top, other_half(top)), c, -T::kLift);
+      top = kByBlock ? max2(top, other_half(top)) - P::kLift : fmaf(max2(top, other_half(top)), c, -P::kLift);
       if (__any(top > m[n] + kSlack)) {
         const float m_new = fmaxf(m[n], top);
         const float alpha = m_new == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(m[n] - m_new);
@@ -870,21 +914,21 @@ __global__ __launch_bounds__(256, D * NC <= 128 ? 2 : 1) void k_attn_rows(AttnAr
       }
 #pragma unroll
       for (int e = 0; e < kSteps; ++e)
-        p[n][e] = make_uint4(T::pack(s[n][2 * e][0], s[n][2 * e][1]), T::pack(s[n][2 * e][2], s[n][2 * e][3]),
-                             T::pack(s[n][2 * e + 1][0], s[n][2 * e + 1][1]), T::pack(s[n][2 * e + 1][2], s[n][2 * e + 1][3]));
+        p[n][e] = make_uint4(P::pack(s[n][2 * e][0], s[n][2 * e][1]), P::pack(s[n][2 * e][2], s[n][2 * e][3]),
+                             P::pack(s[n][2 * e + 1][0], s[n][2 * e + 1][1]), P::pack(s[n][2 * e + 1][2], s[n][2 * e + 1][3]));
     }
     uint32_t any = 0;
 #pragma unroll
     for (int i = 0; i < D / 16; ++i)
 #pragma unroll
       for (int e = 0; e < kSteps; ++e) {
-        uint4 v = k8 ? e ? widen8<T, kKind>(vf[i].z, vf[i].w) : widen8<T, kKind>(vf[i].x, vf[i].y) : vf[i];
+        uint4 v = k8 ? e ? widen8<P, kKind>(vf[i].z, vf[i].w) : widen8<P, kKind>(vf[i].x, vf[i].y) : vf[i];
         if (!kFinite && edge) {
           any |= not_finite<T>(v);
           v = finite_part<T>(v);
         }
 #pragma unroll
-        for (int n = 0; n < NC; ++n) o[n][i] = T::mfma16(v, p[n][e], o[n][i]);
+        for (int n = 0; n < NC; ++n) o[n][i] = P::mfma16(v, p[n][e], o[n][i]);
         if (NC > 1 && e == kSteps - 1) __builtin_amdgcn_sched_barrier(0);
       }
     // Of a key that some query sees?  (A block's unused end may hold anything; a
