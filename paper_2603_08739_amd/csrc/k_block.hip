@@ -102,6 +102,19 @@ __device__ __forceinline__ uint32_t shrink4(uint32_t u, float by) {
   return H::pack4(f[0] * by, f[1] * by, f[2] * by, f[3] * by);
 }
 
+// byte (16 bits: half) i of the result's word j is byte j of word i
+__device__ __forceinline__ void turn_bytes(uint32_t* u) {
+  const uint32_t a = __builtin_amdgcn_perm(u[1], u[0], 0x05010400u), b = __builtin_amdgcn_perm(u[3], u[2], 0x05010400u);
+  const uint32_t c = __builtin_amdgcn_perm(u[1], u[0], 0x07030602u), d = __builtin_amdgcn_perm(u[3], u[2], 0x07030602u);
+  u[0] = __builtin_amdgcn_perm(b, a, 0x05040100u), u[1] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+  u[2] = __builtin_amdgcn_perm(d, c, 0x05040100u), u[3] = __builtin_amdgcn_perm(d, c, 0x07060302u);
+}
+__device__ __forceinline__ void turn_halves(uint32_t& a, uint32_t& b) {
+  const uint32_t lo = __builtin_amdgcn_perm(b, a, 0x05040100u);
+  b = __builtin_amdgcn_perm(b, a, 0x07060302u);
+  a = lo;
+}
+
 // Infinities and NaN do not make a scale.
 __device__ __forceinline__ float magnitude_of(float x) {
   const uint32_t u = __builtin_bit_cast(uint32_t, x) & 0x7fffffffu;
@@ -148,19 +161,26 @@ struct BlockArgs {
   int64_t k_block, v_block;
   float *k_scale, *v_scale;
   uint64_t slots;  // n_blocks * block_size
-  uint32_t max_tokens, q_heads, kv_heads, dim, units, rot_dim, heads_each, q_groups;
+  uint32_t max_tokens, q_heads, kv_heads, dim_shift, units, rot_dim, heads_each, q_groups;
   uint32_t q_blocks;  // workgroups of queries; the rest take runs
+  uint32_t waves;     // of a task
+  uint32_t tasks;     // runs by heads by keys or values
   float magnitude;
 };
 
-constexpr int kStrip = 64;  // elements of V turned through LDS at a time
-
-template <class V, bool kHalf, class H>
-__global__ __launch_bounds__(256) void k_append_block(BlockArgs a) {
-  const int tid = threadIdx.x;
+// A task is a run's keys of one head, or its values: a wavefront for up to 2,048 of
+// a block's numbers, up to 16 of them together.  What goes into the block stays in
+// registers from its largest magnitude to its rounding, so everything is read and written
+// once.
+//   keys     a lane has 16 elements of kItems tokens, turned
+//   values   8 elements of 4 tokens, kItems / 2 times, turned to 4 tokens of 8
+//            elements in registers; words that other tokens share are read first
+template <class V, bool kHalf, class H, int kItems>
+__global__ void __launch_bounds__(1024) k_append_block(BlockArgs a) {
+  const uint32_t tid = threadIdx.x;
   if (blockIdx.x < a.q_blocks) {  // queries: as in k_append
     const uint32_t n_tokens = min((uint32_t)max(a.runs.start[a.runs.n_req], 0), a.max_tokens);
-    const uint64_t id = (uint64_t)blockIdx.x * 256 + tid;
+    const uint64_t id = (uint64_t)blockIdx.x * blockDim.x + tid;
     const uint32_t unit = (uint32_t)(id % a.units);
     const uint64_t rest = id / a.units;
     const uint32_t group = (uint32_t)(rest % a.q_groups);
@@ -176,117 +196,176 @@ __global__ __launch_bounds__(256) void k_append_block(BlockArgs a) {
     return;
   }
 
-  const uint32_t id = blockIdx.x - a.q_blocks, head = id % a.kv_heads;
+  // All wavefronts of a task leave together or not at all: there is a barrier below.
+  const bool alone = a.waves == 1;
+  const uint32_t me = alone ? lane_id() : tid, threads = a.waves * 64;
+  const uint32_t task = alone ? (blockIdx.x - a.q_blocks) * (blockDim.x / 64) + wave_id() : blockIdx.x - a.q_blocks;
+  if (task >= a.tasks) return;
+  const bool keys = !(task & 1);
+  const uint32_t place = task / 2 / a.kv_heads, head = task / 2 - place * a.kv_heads;
   uint32_t req, run;
-  find_run(a.runs, id / a.kv_heads, req, run);
+  find_run(a.runs, place, req, run);
   if (req >= a.runs.n_req) return;
-  const int64_t size = 1ll << a.runs.shift;
-  const int64_t t0 = a.runs.start[req], t1 = min((int64_t)a.runs.start[req + 1], (int64_t)a.max_tokens);
+  const uint32_t shift = a.runs.shift;
+  const int64_t t0 = a.runs.start[req], end = a.runs.start[req + 1], t1 = min(end, (int64_t)a.max_tokens);
   if (t0 < 0 || t0 >= t1) return;
   // the run: n tokens from `token` on, in places `at` and on of their block
-  const int64_t ctx = a.kv_len[req] - ((int64_t)a.runs.start[req + 1] - t0);
+  const int64_t ctx = a.kv_len[req] - (end - t0);
   if (ctx < 0) return;
-  const int64_t block0 = ((ctx >> a.runs.shift) + run) << a.runs.shift;
-  const int64_t from = max(ctx, block0), to = min(ctx + (t1 - t0), block0 + size);
+  const int64_t block0 = ((ctx >> shift) + run) << shift;
+  const int64_t from = max(ctx, block0), to = min(ctx + (t1 - t0), block0 + (1ll << shift));
   if (from >= to) return;
   const uint32_t token = (uint32_t)(t0 + (from - ctx)), n = (uint32_t)(to - from), at = (uint32_t)(from - block0);
   const int64_t slot = a.slot[token];
   if (slot < 0 || (uint64_t)slot >= a.slots) return;
-  const int64_t page = slot >> a.runs.shift;
+  const int64_t page = slot >> shift;
+  float* const scales = (keys ? a.k_scale : a.v_scale) + page * a.kv_heads + head;
+  const float old = at ? *scales : 0.0f;
 
-  const uint16_t* k = a.k + (int64_t)token * a.kt + head * a.kh;
-  const uint16_t* v = a.v + (int64_t)token * a.vt + head * a.vh;
-  // a thread's 16 elements of a key: item = token * units + unit
-  auto key = [&](uint32_t item, float* f, float* g, int& lo, int& hi) {
-    const uint32_t t = item / a.units, unit = item - t * a.units;
+  __shared__ uint32_t most[16];
+  // the largest magnitude of the task's elements, and what it makes of the scale
+  auto scale_of = [&](float mine) {
+    uint32_t u = (uint32_t)__builtin_amdgcn_readlane((int)wave_incl_max_u32(__builtin_bit_cast(uint32_t, mine)), 63);
+    if (!alone) {
+      if (lane_id() == 0) most[wave_id()] = u;
+      __syncthreads();
+      u = most[0];
+      for (uint32_t w = 1; w < a.waves; ++w) u = max(u, most[w]);
+    }
+    // A need that is not 0 is no subnormal number: new_scale() reads exponents.
+    const float x = __builtin_bit_cast(float, u) / H::kMost;
+    const NewScale s = new_scale(x > 0.0f ? fmaxf(x, 0x1p-126f) : 0.0f, old);
+    if (me == 0) *scales = s.scale;
+    return s;
+  };
+
+  if (keys) {
+    uint8_t* const kc = a.kc + page * a.k_block + ((int64_t)head << (shift + a.dim_shift));
+    const uint32_t unit_shift = a.dim_shift - 4, unit = me & (a.units - 1);
+    int lo, hi;
     unit_at<kHalf>(unit, a.rot_dim, lo, hi);
-    const uint16_t* p = k + (int64_t)t * a.kt;
-    unpack<V>(*(const uint4*)(p + lo), f);
-    unpack<V>(*(const uint4*)(p + hi), g);
-    if (unit < a.rot_dim / 16) {
-      Turns turns;
-      load_turns(turns, a.turn, unit, a.pos[token + t], 1.0f, a.magnitude);
-      turn_unit<kHalf>(f, g, turns);
+    const bool turns = unit < a.rot_dim / 16;
+    const uint16_t* const k = a.k + (int64_t)token * a.kt + head * a.kh;
+    float f[kItems][8], g[kItems][8];
+    uint4 u[kItems], w[kItems];
+    int32_t pos[kItems];
+    // (units divide a task's threads: a lane's items are those of one unit)
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      const uint32_t t = (me + i * threads) >> unit_shift;
+      u[i] = w[i] = make_uint4(0, 0, 0, 0);
+      pos[i] = 0;
+      if (t < n) {
+        u[i] = *(const uint4*)(k + (int64_t)t * a.kt + lo);
+        w[i] = *(const uint4*)(k + (int64_t)t * a.kt + hi);
+        if (turns) pos[i] = a.pos[token + t];
+      }
     }
-    return t;
-  };
-
-  // the largest magnitudes
-  float most_k = 0.0f, most_v = 0.0f;
-  for (uint32_t item = tid; item < n * a.units; item += 256) {
-    float f[8], g[8];
-    int lo, hi;
-    key(item, f, g, lo, hi);
+    float mine = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) most_k = fmaxf(most_k, fmaxf(magnitude_of(f[i]), magnitude_of(g[i])));
-  }
-  for (uint32_t item = tid; item < n * a.units * 2; item += 256) {
-    const uint32_t t = item / (a.units * 2), chunk = item - t * a.units * 2;
-    float f[8];
-    unpack<V>(*(const uint4*)(v + (int64_t)t * a.vt + chunk * 8), f);
+    for (int i = 0; i < kItems; ++i) {
+      unpack<V>(u[i], f[i]);
+      unpack<V>(w[i], g[i]);
+      if (turns && (me + i * threads) >> unit_shift < n) {
+        Turns t;
+        load_turns(t, a.turn, unit, pos[i], 1.0f, a.magnitude);
+        turn_unit<kHalf>(f[i], g[i], t);
+      }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) most_v = fmaxf(most_v, magnitude_of(f[i]));
-  }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) most_k = fmaxf(most_k, __shfl_xor(most_k, d, 64)), most_v = fmaxf(most_v, __shfl_xor(most_v, d, 64));
-  __shared__ float most[2][4];
-  if (lane_id() == 0) most[0][wave_id()] = most_k, most[1][wave_id()] = most_v;
-  const int64_t scale_at = page * a.kv_heads + head;
-  const float old_k = at ? a.k_scale[scale_at] : 0.0f, old_v = at ? a.v_scale[scale_at] : 0.0f;
-  __syncthreads();
-  // A need that is not 0 is no subnormal number: new_scale() reads exponents.
-  auto need = [&](const float* m) {
-    const float x = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) / H::kMost;
-    return x > 0.0f ? fmaxf(x, 0x1p-126f) : 0.0f;
-  };
-  const NewScale sk = new_scale(need(most[0]), old_k), sv = new_scale(need(most[1]), old_v);
-  if (tid == 0) a.k_scale[scale_at] = sk.scale, a.v_scale[scale_at] = sv.scale;
-
-  // keys
-  uint8_t* kc = a.kc + page * a.k_block + ((int64_t)head << a.runs.shift) * a.dim;
-  for (uint32_t item = tid; item < n * a.units; item += 256) {
-    float f[8], g[8];
-    int lo, hi;
-    const uint32_t t = key(item, f, g, lo, hi);
-    uint8_t* to_row = kc + (int64_t)(at + t) * a.dim;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] *= sk.inverse, g[i] *= sk.inverse;
-    *(uint2*)(to_row + lo) = make_uint2(H::pack4(f[0], f[1], f[2], f[3]), H::pack4(f[4], f[5], f[6], f[7]));
-    *(uint2*)(to_row + hi) = make_uint2(H::pack4(g[0], g[1], g[2], g[3]), H::pack4(g[4], g[5], g[6], g[7]));
-  }
-  if (at && sk.shrink != 1.0f)
-    for (uint32_t i = tid; i < at * a.dim / 4; i += 256) {
-      uint32_t* p = (uint32_t*)kc + i;
-      *p = shrink4<H>(*p, sk.shrink);
+      for (int e = 0; e < 8; ++e) mine = fmaxf(mine, fmaxf(magnitude_of(f[i][e]), magnitude_of(g[i][e])));
     }
+    const NewScale s = scale_of(mine);
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      const uint32_t t = (me + i * threads) >> unit_shift;
+      if (t >= n) continue;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[i][e] *= s.inverse, g[i][e] *= s.inverse;
+      uint8_t* row = kc + ((int64_t)(at + t) << a.dim_shift);
+      *(uint2*)(row + lo) = make_uint2(H::pack4(f[i][0], f[i][1], f[i][2], f[i][3]), H::pack4(f[i][4], f[i][5], f[i][6], f[i][7]));
+      *(uint2*)(row + hi) = make_uint2(H::pack4(g[i][0], g[i][1], g[i][2], g[i][3]), H::pack4(g[i][4], g[i][5], g[i][6], g[i][7]));
+    }
+    if (at && s.shrink != 1.0f)
+      for (uint32_t i = me; i < at << (a.dim_shift - 4); i += threads) {
+        uint4* p = (uint4*)kc + i;
+        const uint4 x = *p;
+        *p = make_uint4(shrink4<H>(x.x, s.shrink), shrink4<H>(x.y, s.shrink), shrink4<H>(x.z, s.shrink), shrink4<H>(x.w, s.shrink));
+      }
+    return;
+  }
 
-  // values: a strip of elements through LDS, then along the tokens
-  uint8_t* vc = a.vc + page * a.v_block + ((int64_t)head * a.dim << a.runs.shift);
-  __shared__ uint8_t strip[kStrip][256 + 4];
-  for (uint32_t d0 = 0; d0 < a.dim; d0 += kStrip) {
-    __syncthreads();
-    for (uint32_t item = tid; item < n * (kStrip / 8); item += 256) {
-      const uint32_t t = item / (kStrip / 8), chunk = item % (kStrip / 8);
+  uint8_t* const vc = a.vc + page * a.v_block + ((int64_t)head << (shift + a.dim_shift));
+  const uint32_t chunk_shift = a.dim_shift - 3, d = (me & ((1u << chunk_shift) - 1)) * 8;
+  const uint16_t* const v = a.v + (int64_t)token * a.vt + head * a.vh + d;
+  constexpr int kWords = kItems / 2;
+  uint4 x[kWords][4];
+  uint32_t before[kWords][8];
+  // places p .. p + 3 of the block; bytes of those that the run fills
+  auto place_of = [&](int i) { return ((me + i * threads) >> chunk_shift) * 4; };
+  auto bytes_in = [](int first, int last) {  // of places `first` to `last` - 1 of four
+    const uint32_t below = last >= 4 ? 0xffffffffu : last > 0 ? (1u << (8 * last)) - 1 : 0u;
+    return first <= 0 ? below : first >= 4 ? 0u : below & ~((1u << (8 * first)) - 1);
+  };
+#pragma unroll
+  for (int i = 0; i < kWords; ++i) {
+    const uint32_t p = place_of(i);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      x[i][j] = make_uint4(0, 0, 0, 0);
+      if (p + j >= at && p + j < at + n) x[i][j] = *(const uint4*)(v + (int64_t)(p + j - at) * a.vt);
+    }
+    const uint32_t fills = bytes_in((int)at - (int)p, (int)(at + n) - (int)p);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) before[i][e] = 0;
+    if (fills && fills != 0xffffffffu)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) before[i][e] = *(const uint32_t*)(vc + ((int64_t)(d + e) << shift) + p);
+  }
+  float mine = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kWords; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
       float f[8];
-      unpack<V>(*(const uint4*)(v + (int64_t)t * a.vt + d0 + chunk * 8), f);
+      unpack<V>(x[i][j], f);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] *= sv.inverse;
-      const uint32_t lo = H::pack4(f[0], f[1], f[2], f[3]), hi = H::pack4(f[4], f[5], f[6], f[7]);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) strip[chunk * 8 + i][t] = (uint8_t)(lo >> (8 * i)), strip[chunk * 8 + 4 + i][t] = (uint8_t)(hi >> (8 * i));
+      for (int e = 0; e < 8; ++e) mine = fmaxf(mine, magnitude_of(f[e]));
     }
-    __syncthreads();
-    for (uint32_t i = tid; i < n * kStrip; i += 256) {
-      const uint32_t d = i / n, t = i - d * n;
-      vc[((int64_t)(d0 + d) << a.runs.shift) + at + t] = strip[d][t];
+  const NewScale s = scale_of(mine);
+#pragma unroll
+  for (int i = 0; i < kWords; ++i) {
+    const uint32_t p = place_of(i);
+    const uint32_t fills = bytes_in((int)at - (int)p, (int)(at + n) - (int)p);
+    const uint32_t shrinks = s.shrink != 1.0f && p < 1u << shift ? bytes_in(0, (int)at - (int)p) : 0u;
+    if (!fills && !shrinks) continue;
+    uint8_t* const to_words = vc + ((int64_t)d << shift) + p;
+    if (!fills)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) before[i][e] = *(const uint32_t*)(to_words + ((int64_t)e << shift));
+    uint32_t lo[4], hi[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float f[8];
+      unpack<V>(x[i][j], f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] *= s.inverse;
+      lo[j] = H::pack4(f[0], f[1], f[2], f[3]);
+      hi[j] = H::pack4(f[4], f[5], f[6], f[7]);
+    }
+    turn_bytes(lo);
+    turn_bytes(hi);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      uint32_t* const word = (uint32_t*)(to_words + ((int64_t)e << shift));
+      uint32_t u = e < 4 ? lo[e & 3] : hi[e & 3];
+      if (fills != 0xffffffffu) {
+        uint32_t b = before[i][e];
+        if (shrinks) b = (shrink4<H>(b, s.shrink) & shrinks) | (b & ~shrinks);
+        u = (u & fills) | (b & ~fills);
+      }
+      *word = u;
     }
   }
-  if (at && sv.shrink != 1.0f)
-    for (uint32_t i = tid; i < at * a.dim; i += 256) {
-      const uint32_t d = i / at, t = i - d * at;
-      uint8_t* p = vc + ((int64_t)d << a.runs.shift) + t;
-      *p = (uint8_t)shrink4<H>(*p, sv.shrink);
-    }
 }
 
 // ---------------------------------------------------------------------------
@@ -319,19 +398,6 @@ __device__ __forceinline__ uint2 rows4(uint32_t u, float by) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) h[i] = __builtin_bit_cast(uint16_t, (E)(f[i] * by));
   return make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
-}
-
-// byte (16 bits: half) i of the result's word j is byte j of word i
-__device__ __forceinline__ void turn_bytes(uint32_t* u) {
-  const uint32_t a = __builtin_amdgcn_perm(u[1], u[0], 0x05010400u), b = __builtin_amdgcn_perm(u[3], u[2], 0x05010400u);
-  const uint32_t c = __builtin_amdgcn_perm(u[1], u[0], 0x07030602u), d = __builtin_amdgcn_perm(u[3], u[2], 0x07030602u);
-  u[0] = __builtin_amdgcn_perm(b, a, 0x05040100u), u[1] = __builtin_amdgcn_perm(b, a, 0x07060302u);
-  u[2] = __builtin_amdgcn_perm(d, c, 0x05040100u), u[3] = __builtin_amdgcn_perm(d, c, 0x07060302u);
-}
-__device__ __forceinline__ void turn_halves(uint32_t& a, uint32_t& b) {
-  const uint32_t lo = __builtin_amdgcn_perm(b, a, 0x05040100u);
-  b = __builtin_amdgcn_perm(b, a, 0x07060302u);
-  a = lo;
 }
 
 // A wavefront reads 8 KB of a run's keys, or of its values, whatever heads these are: it
@@ -459,11 +525,11 @@ __global__ __launch_bounds__(256) void k_read(ReadArgs a) {
 }
 
 template <class V, class H>
-void launch_append(const BlockArgs& a, bool half, uint32_t grid, hipStream_t s) {
-  if (half)
-    hipLaunchKernelGGL((k_append_block<V, true, H>), dim3(grid), dim3(256), 0, s, a);
-  else
-    hipLaunchKernelGGL((k_append_block<V, false, H>), dim3(grid), dim3(256), 0, s, a);
+void launch_append(const BlockArgs& a, bool half, bool more, uint32_t grid, uint32_t threads, hipStream_t s) {
+  if (half && !more) hipLaunchKernelGGL((k_append_block<V, true, H, 2>), dim3(grid), dim3(threads), 0, s, a);
+  if (half && more) hipLaunchKernelGGL((k_append_block<V, true, H, 4>), dim3(grid), dim3(threads), 0, s, a);
+  if (!half && !more) hipLaunchKernelGGL((k_append_block<V, false, H, 2>), dim3(grid), dim3(threads), 0, s, a);
+  if (!half && more) hipLaunchKernelGGL((k_append_block<V, false, H, 4>), dim3(grid), dim3(threads), 0, s, a);
 }
 
 template <class V>
@@ -497,20 +563,26 @@ kv_status paged_append_block(const kv_paged_batch& b, const kv_paged_cache& c, c
   a.slots = (uint64_t)c.n_blocks * b.block_size;
   a.max_tokens = b.max_tokens;
   a.q_heads = q.ptr ? b.q_heads : 0, a.kv_heads = b.kv_heads;
-  a.dim = b.head_dim, a.units = b.head_dim / 16;
+  a.dim_shift = (uint32_t)__builtin_ctz(b.head_dim), a.units = b.head_dim / 16;
   a.heads_each = heads_each_for((uint64_t)b.max_tokens * a.q_heads * a.units);
   a.q_groups = (a.q_heads + a.heads_each - 1) / a.heads_each;
-  const uint64_t qs = ((uint64_t)b.max_tokens * a.q_groups * a.units + 255) / 256;
-  const uint64_t runs = plan_runs(a.runs, b.q_start, b.n_req, b.block_size, b.max_tokens,
-                                  b.max_new ? std::min(b.max_new, b.max_tokens) : b.max_tokens) * b.kv_heads;
-  if (qs + runs > 0x7fffffffull) return fail(KV_ERR_UNSUPPORTED, "kv_paged_append: too many heads for one call");
-  a.q_blocks = (uint32_t)qs;
-  const uint32_t grid = (uint32_t)(qs + runs);
+  const uint32_t numbers = b.block_size * b.head_dim;
+  a.waves = std::min(std::max(numbers / 2048, 1u), 16u);
+  const bool more = numbers > 32768;  // 4,096 of a block's numbers to a wavefront
+  const uint32_t threads = a.waves == 1 ? 256 : a.waves * 64;
+  const uint64_t qs = ((uint64_t)b.max_tokens * a.q_groups * a.units + threads - 1) / threads;
+  const uint64_t tasks = plan_runs(a.runs, b.q_start, b.n_req, b.block_size, b.max_tokens,
+                                   b.max_new ? std::min(b.max_new, b.max_tokens) : b.max_tokens) * b.kv_heads * 2;
+  const uint64_t groups = a.waves == 1 ? (tasks + 3) / 4 : tasks;
+  if (tasks > 0x7fffffffull || qs + groups > 0x7fffffffull || (qs + groups) * threads > 0xffffffffull)
+    return fail(KV_ERR_UNSUPPORTED, "kv_paged_append: too many heads for one call");
+  a.tasks = (uint32_t)tasks, a.q_blocks = (uint32_t)qs;
+  const uint32_t grid = (uint32_t)(qs + groups);
   const bool half = !r || r->layout == KV_ROPE_HALF, i8 = c.dtype == KV_DT_I8_BLOCK;
   if (dtype == KV_DT_BF16)
-    i8 ? launch_append<bf16x8, I8>(a, half, grid, s) : launch_append<bf16x8, Fp8>(a, half, grid, s);
+    i8 ? launch_append<bf16x8, I8>(a, half, more, grid, threads, s) : launch_append<bf16x8, Fp8>(a, half, more, grid, threads, s);
   else
-    i8 ? launch_append<f16x8, I8>(a, half, grid, s) : launch_append<f16x8, Fp8>(a, half, grid, s);
+    i8 ? launch_append<f16x8, I8>(a, half, more, grid, threads, s) : launch_append<f16x8, Fp8>(a, half, more, grid, threads, s);
   KV_HIP(hipGetLastError());
   return KV_OK;
 }
