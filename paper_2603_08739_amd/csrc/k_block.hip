@@ -44,25 +44,43 @@ uint64_t plan_runs(Runs& r, const int32_t* start, uint32_t n_req, uint32_t block
   return direct ? one * n_req : found;
 }
 
-// The request of place u and which of its runs it is; the whole wavefront asks.
-__device__ __forceinline__ void find_run(const Runs& runs, uint32_t u, uint32_t& req, uint32_t& run) {
+struct Run {
+  uint32_t req, run;        // the request, n_req: none; which of its runs
+  int32_t start, end;       // its tokens
+  int32_t length, first;    // kv_len, and the first position asked for (NULL: 0)
+};
+
+// The run of place u; the whole wavefront asks.  What is known of a request is loaded
+// by the lane that has it as its candidate, all at once: a small step is one chain of such
+// round trips.
+__device__ __forceinline__ Run find_run(const Runs& runs, uint32_t u, const int32_t* length, const int32_t* first) {
+  Run r;
   if (runs.each) {
-    req = u / runs.each;
-    run = u - req * runs.each;
-    return;
+    r.req = u / runs.each;
+    r.run = u - r.req * runs.each;
+    const uint32_t at = min(r.req, runs.n_req - 1);
+    r.start = runs.start[at], r.end = runs.start[at + 1], r.length = length[at], r.first = first ? first[at] : 0;
+    return r;
   }
-  auto base = [&](uint32_t r) { return ((uint32_t)max(runs.start[r], 0) >> runs.shift) + 2 * r; };
+  auto base = [&](int32_t start, uint32_t req) { return ((uint32_t)max(start, 0) >> runs.shift) + 2 * req; };
   uint32_t lo = 0, n = runs.n_req;
-  while (n > 1) {
+  while (n > 64) {
     const uint32_t step = (n + 63) / 64, at = lane_id() * step;
-    const uint64_t below = __ballot(at < n && base(lo + min(at, n - 1)) <= u);
+    const uint64_t below = __ballot(at < n && base(runs.start[lo + min(at, n - 1)], lo + at) <= u);
     const uint32_t i = (uint32_t)max((int)__popcll(below) - 1, 0) * step;
     lo += i;
     n = min(step, n - i);
   }
-  const uint32_t mine = base(lo);
-  req = mine <= u ? lo : runs.n_req;  // (a first row that is not 0 leaves the places before it to nobody)
-  run = u - mine;
+  const uint32_t at = lo + min(lane_id(), n - 1);
+  const int32_t start = runs.start[at], end = runs.start[at + 1], len = length[at], from = first ? first[at] : 0;
+  const uint64_t below = __ballot(lane_id() < n && base(start, at) <= u);
+  const int i = max((int)__popcll(below) - 1, 0);
+  r.start = __builtin_amdgcn_readlane(start, i), r.end = __builtin_amdgcn_readlane(end, i);
+  r.length = __builtin_amdgcn_readlane(len, i), r.first = __builtin_amdgcn_readlane(from, i);
+  // (a first row that is not 0 leaves the places before it to nobody)
+  r.req = below ? lo + i : runs.n_req;
+  r.run = u - base(r.start, lo + i);
+  return r;
 }
 
 // ---------------------------------------------------------------------------
@@ -203,28 +221,27 @@ __global__ void __launch_bounds__(1024) k_append_block(BlockArgs a) {
   if (task >= a.tasks) return;
   const bool keys = !(task & 1);
   const uint32_t place = task / 2 / a.kv_heads, head = task / 2 - place * a.kv_heads;
-  uint32_t req, run;
-  find_run(a.runs, place, req, run);
-  if (req >= a.runs.n_req) return;
+  const Run r = find_run(a.runs, place, a.kv_len, nullptr);
+  if (r.req >= a.runs.n_req) return;
   const uint32_t shift = a.runs.shift;
-  const int64_t t0 = a.runs.start[req], end = a.runs.start[req + 1], t1 = min(end, (int64_t)a.max_tokens);
+  const int64_t t0 = r.start, t1 = min((int64_t)r.end, (int64_t)a.max_tokens);
   if (t0 < 0 || t0 >= t1) return;
   // the run: n tokens from `token` on, in places `at` and on of their block
-  const int64_t ctx = a.kv_len[req] - (end - t0);
+  const int64_t ctx = r.length - ((int64_t)r.end - t0);
   if (ctx < 0) return;
-  const int64_t block0 = ((ctx >> shift) + run) << shift;
+  const int64_t block0 = ((ctx >> shift) + r.run) << shift;
   const int64_t from = max(ctx, block0), to = min(ctx + (t1 - t0), block0 + (1ll << shift));
   if (from >= to) return;
   const uint32_t token = (uint32_t)(t0 + (from - ctx)), n = (uint32_t)(to - from), at = (uint32_t)(from - block0);
   const int64_t slot = a.slot[token];
-  if (slot < 0 || (uint64_t)slot >= a.slots) return;
-  const int64_t page = slot >> shift;
+  // (looked at when the elements are on their way)
+  const bool there = slot >= 0 && (uint64_t)slot < a.slots;
+  const int64_t page = there ? slot >> shift : 0;
   float* const scales = (keys ? a.k_scale : a.v_scale) + page * a.kv_heads + head;
-  const float old = at ? *scales : 0.0f;
 
   __shared__ uint32_t most[16];
   // the largest magnitude of the task's elements, and what it makes of the scale
-  auto scale_of = [&](float mine) {
+  auto scale_of = [&](float mine, float old) {
     uint32_t u = (uint32_t)__builtin_amdgcn_readlane((int)wave_incl_max_u32(__builtin_bit_cast(uint32_t, mine)), 63);
     if (!alone) {
       if (lane_id() == 0) most[wave_id()] = u;
@@ -261,6 +278,8 @@ __global__ void __launch_bounds__(1024) k_append_block(BlockArgs a) {
         if (turns) pos[i] = a.pos[token + t];
       }
     }
+    if (!there) return;
+    const float old = at ? *scales : 0.0f;
     float mine = 0.0f;
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
@@ -274,7 +293,7 @@ __global__ void __launch_bounds__(1024) k_append_block(BlockArgs a) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) mine = fmaxf(mine, fmaxf(magnitude_of(f[i][e]), magnitude_of(g[i][e])));
     }
-    const NewScale s = scale_of(mine);
+    const NewScale s = scale_of(mine, old);
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
       const uint32_t t = (me + i * threads) >> unit_shift;
@@ -314,6 +333,12 @@ __global__ void __launch_bounds__(1024) k_append_block(BlockArgs a) {
       x[i][j] = make_uint4(0, 0, 0, 0);
       if (p + j >= at && p + j < at + n) x[i][j] = *(const uint4*)(v + (int64_t)(p + j - at) * a.vt);
     }
+  }
+  if (!there) return;
+  const float old = at ? *scales : 0.0f;
+#pragma unroll
+  for (int i = 0; i < kWords; ++i) {
+    const uint32_t p = place_of(i);
     const uint32_t fills = bytes_in((int)at - (int)p, (int)(at + n) - (int)p);
 #pragma unroll
     for (int e = 0; e < 8; ++e) before[i][e] = 0;
@@ -331,7 +356,7 @@ __global__ void __launch_bounds__(1024) k_append_block(BlockArgs a) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) mine = fmaxf(mine, magnitude_of(f[e]));
     }
-  const NewScale s = scale_of(mine);
+  const NewScale s = scale_of(mine, old);
 #pragma unroll
   for (int i = 0; i < kWords; ++i) {
     const uint32_t p = place_of(i);
@@ -387,6 +412,15 @@ struct ReadArgs {
 
 // 16-bit caches: numbers are copied
 struct Same {};
+// 8 numbers
+template <int kBytes>
+struct Load {
+  typedef uint4 type;
+};
+template <>
+struct Load<1> {
+  typedef uint2 type;
+};
 
 // 4 numbers, times their scale, in 16 bits
 template <class V, class H>
@@ -398,6 +432,13 @@ __device__ __forceinline__ uint2 rows4(uint32_t u, float by) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) h[i] = __builtin_bit_cast(uint16_t, (E)(f[i] * by));
   return make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
+}
+
+// Rows are written past the caches, which they would fill with what nobody reads twice (64
+// prefixes, 417 MB read and written: 67 us, with plain stores 93).
+__device__ __forceinline__ void put_row(uint16_t* p, const uint4& w) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  __builtin_nontemporal_store(__builtin_bit_cast(u32x4, w), (u32x4*)p);
 }
 
 // A wavefront reads 8 KB of a run's keys, or of its values, whatever heads these are: it
@@ -414,23 +455,22 @@ __global__ __launch_bounds__(256) void k_read(ReadArgs a) {
   if (task >= a.tasks) return;
   const uint32_t place = task / (2 * a.each);
   uint32_t part = task - place * (2 * a.each);
-  uint32_t req, run;
-  find_run(a.runs, place, req, run);
-  if (req >= a.runs.n_req) return;
+  const Run r = find_run(a.runs, place, a.kv_len, a.first);
+  if (r.req >= a.runs.n_req) return;
   const uint32_t shift = a.runs.shift;
-  const int64_t t0 = a.runs.start[req], t1 = min((int64_t)a.runs.start[req + 1], (int64_t)a.max_rows);
+  const int64_t t0 = r.start, t1 = min((int64_t)r.end, (int64_t)a.max_rows);
   if (t0 < 0 || t0 >= t1) return;
-  const int64_t first = a.first ? a.first[req] : 0;
-  const int64_t column = (first >> shift) + run, block0 = column << shift;
+  const int64_t first = r.first;
+  const int64_t column = (first >> shift) + r.run, block0 = column << shift;
   const int64_t from = max(first, block0), to = min(first + (t1 - t0), block0 + (1ll << shift));
   if (from >= to) return;
   // Places begin .. end - 1 of the block are rows, those before `have` are in the cache.
   const uint32_t begin = (uint32_t)(from - block0), end = (uint32_t)(to - block0);
   const int64_t row0 = t0 + (from - first) - begin;  // row of place 0
   int page = -1;
-  if (column >= 0 && column < a.max_blocks) page = a.table[(uint64_t)req * a.max_blocks + column];
+  if (column >= 0 && column < a.max_blocks) page = a.table[(uint64_t)r.req * a.max_blocks + column];
   const bool there = page >= 0 && page < (int)a.n_blocks;
-  const uint32_t have = there ? (uint32_t)min(max((int64_t)a.kv_len[req] - block0, (int64_t)0), (int64_t)end) : 0;
+  const uint32_t have = there ? (uint32_t)min(max((int64_t)r.length - block0, (int64_t)0), (int64_t)end) : 0;
   if (!there) page = 0;
   const bool keys = part < a.each;
   if (!keys) part -= a.each;
@@ -443,40 +483,39 @@ __global__ __launch_bounds__(256) void k_read(ReadArgs a) {
   if (keys) {
     const uint8_t* kc = a.kc + page * a.k_block;
     constexpr int kSteps = 16 / kBytes;  // of 64 lanes by 8 elements
-    constexpr int kAhead = 8;
     const uint32_t chunk_shift = a.dim_shift - 3;
-#pragma unroll 1
-    for (int step = 0; step < kSteps; step += kAhead) {
-      uint4 u[kAhead];
-      float by[kAhead];
-      uint32_t at[kAhead];
+    typedef typename Load<kBytes>::type U;
+    U u[kSteps];
+    float by[kSteps];
+    auto item = [&](int i, uint32_t& t, uint32_t& head) {
+      const uint32_t at = (part * kSteps + i) * 64 + lane;
+      t = (at >> chunk_shift) & ((1u << shift) - 1), head = at >> (chunk_shift + shift);
+      return at;
+    };
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        at[i] = (part * kSteps + step + i) * 64 + lane;
-        const uint32_t t = (at[i] >> chunk_shift) & ((1u << shift) - 1), head = at[i] >> (chunk_shift + shift);
-        u[i] = make_uint4(0, 0, 0, 0);
-        by[i] = 1.0f;
-        if (head < a.kv_heads && t >= begin && t < have) {
-          const uint8_t* p = kc + (int64_t)at[i] * 8 * kBytes;
-          if constexpr (kBytes == 2) {
-            u[i] = *(const uint4*)p;
-          } else {
-            const uint2 w = *(const uint2*)p;
-            u[i].x = w.x, u[i].y = w.y;
-            by[i] = scale_of(head);
-          }
-        }
+    for (int i = 0; i < kSteps; ++i) {
+      uint32_t t, head;
+      const uint32_t at = item(i, t, head);
+      u[i] = U{};
+      by[i] = 1.0f;
+      if (head < a.kv_heads && t >= begin && t < have) {
+        u[i] = *(const U*)(kc + (int64_t)at * 8 * kBytes);
+        by[i] = scale_of(head);
       }
+    }
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const uint32_t t = (at[i] >> chunk_shift) & ((1u << shift) - 1), head = at[i] >> (chunk_shift + shift);
-        if (head >= a.kv_heads || t < begin || t >= end) continue;
-        if constexpr (kBytes == 1) {
-          const uint2 lo = rows4<V, H>(u[i].x, by[i]), hi = rows4<V, H>(u[i].y, by[i]);
-          u[i] = make_uint4(lo.x, lo.y, hi.x, hi.y);
-        }
-        *(uint4*)(a.k + (row0 + t) * a.kt + head * a.kh + (at[i] & ((1u << chunk_shift) - 1)) * 8) = u[i];
+    for (int i = 0; i < kSteps; ++i) {
+      uint32_t t, head;
+      const uint32_t at = item(i, t, head);
+      if (head >= a.kv_heads || t < begin || t >= end) continue;
+      uint4 w;
+      if constexpr (kBytes == 1) {
+        const uint2 lo = rows4<V, H>(u[i].x, by[i]), hi = rows4<V, H>(u[i].y, by[i]);
+        w = make_uint4(lo.x, lo.y, hi.x, hi.y);
+      } else {
+        w = u[i];
       }
+      put_row(a.k + (row0 + t) * a.kt + head * a.kh + (at & ((1u << chunk_shift) - 1)) * 8, w);
     }
     return;
   }
@@ -500,7 +539,7 @@ __global__ __launch_bounds__(256) void k_read(ReadArgs a) {
   uint16_t* out = a.v + (row0 + t) * a.vt + head * a.vh + d;
   auto put = [&](int i, const uint4& w) {
     const uint32_t at = t + i;
-    if (at >= begin && at < end) *(uint4*)(out + i * a.vt) = at < have ? w : make_uint4(0, 0, 0, 0);
+    if (at >= begin && at < end) put_row(out + i * a.vt, at < have ? w : make_uint4(0, 0, 0, 0));
   };
   auto word = [](const uint4& w, int i) { return i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w; };
 #pragma unroll
