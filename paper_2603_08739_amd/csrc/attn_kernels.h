@@ -785,8 +785,8 @@ __global__ __launch_bounds__(256, D * NC <= 128 ? 2 : 1) void k_attn_rows(AttnAr
     now = look_up(first);
     next = look_up(first + 4 * kKeys);
     load_k(first, now.k);
+    if constexpr (kByBlock) load_scales(now.v);  // ahead of the values, which are waited for later
     load_v(first, now.v);
-    if constexpr (kByBlock) load_scales(now.v);
   }
 
   // Queries: operand step s covers the elements that the lane's key loads hold:
@@ -934,9 +934,9 @@ __global__ __launch_bounds__(256, D * NC <= 128 ? 2 : 1) void k_attn_rows(AttnAr
     // Of a key that some query sees?  (A block's unused end may hold anything; a
     // run that only begins among the seen is looked at again below.)
     if (!kFinite && edge) mend = mend || __any(any != 0 && v_ok && key + v_run <= last_pos && key + v_run + kPer > first_pos - window + 1);
-    if (more) load_v(key + 4 * kKeys, next.v);
     if constexpr (kByBlock)
       if (more) load_scales(next.v);
+    if (more) load_v(key + 4 * kKeys, next.v);
     now = next;
     if (key + 8 * kKeys < it.key_end) next = look_up(key + 8 * kKeys);
   }

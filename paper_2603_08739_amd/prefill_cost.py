@@ -10,9 +10,10 @@ its prefix that are cached, brings the rest as new tokens, and the blocks used
 longest ago make room.  Every batch is one serving step of the operators in
 :mod:`.kvpaged`: plan, then for a layer rotation and cache write, then attention.
 
-    python -m paper_2603_08739_amd.prefill_cost --requests 256 --layers 32
+    python -m paper_2603_08739_amd.prefill_cost --requests 256 --layers 32 --cache i8
 
-prints what was measured and the objectives of a small grid under it.
+prints what was measured and the objectives of a small grid under it.  The cache holds 16
+bits or, quantised as it is written, 8.
 """
 from __future__ import annotations
 
@@ -25,6 +26,9 @@ import numpy as np
 import torch
 
 from . import kvpaged
+
+
+KEPT = {"16": None, "fp8": torch.float8_e4m3fn, "i8": torch.int8}  # what a cache may hold
 
 
 class BlockPool:
@@ -100,8 +104,11 @@ def batches(trace, n_blocks, batch):
 
 
 def measure(trace, n_blocks, batch=16, max_requests=None, q_heads=32, kv_heads=8, head_dim=128, dtype=torch.bfloat16,
-            base=500000.0, seed=0, device="cuda"):
-    """Runs the trace's first requests; one layer's seconds and token counts."""
+            base=500000.0, seed=0, device="cuda", kept="16"):
+    """Runs the trace's first requests; one layer's seconds and token counts.  kept: what the
+    cache holds, "16" (dtype), or 8 bits with a scale for each block and head, "fp8" or "i8"."""
+    if kept not in KEPT:
+        raise ValueError(f"kept is {kept!r}; expected one of {', '.join(KEPT)}")
     weights = np.unique(trace.weight)
     if len(weights) != 1:
         raise ValueError("the requests' blocks must have one size")
@@ -110,9 +117,15 @@ def measure(trace, n_blocks, batch=16, max_requests=None, q_heads=32, kv_heads=8
     block = int(trace.tokens_per_granule * weights[0])
     g = torch.Generator(device=device)
     g.manual_seed(seed)
-    k = torch.zeros(n_blocks, kv_heads, block, head_dim, dtype=dtype, device=device)
-    v = torch.zeros(n_blocks, kv_heads, head_dim, block, dtype=dtype, device=device)
-    cache, rope = kvpaged.Cache(k, v), kvpaged.Rope(head_dim, base=base)
+    held = KEPT[kept] or dtype
+    k = torch.zeros(n_blocks, kv_heads, block, head_dim, dtype=held, device=device)
+    v = torch.zeros(n_blocks, kv_heads, head_dim, block, dtype=held, device=device)
+    if KEPT[kept]:
+        scales = [torch.zeros(n_blocks, kv_heads, dtype=torch.float32, device=device) for _ in range(2)]
+        cache = kvpaged.Cache(k, v, *scales, block_scales=True)
+    else:
+        cache = kvpaged.Cache(k, v)
+    rope = kvpaged.Rope(head_dim, base=base)
     i32 = dict(dtype=torch.int32, device=device)
     done = dict(requests=0, steps=0, cached_tokens=0, new_tokens=0, plan_s=0.0, append_s=0.0, attention_s=0.0)
 
@@ -176,11 +189,12 @@ def main(argv=None):
     ap.add_argument("--requests", type=int, default=256)
     ap.add_argument("--batch", type=int, default=16)
     ap.add_argument("--blocks", type=int, default=16384, help="blocks of the HBM cache")
+    ap.add_argument("--cache", choices=sorted(KEPT), default="16", help="what the cache holds: 16 bits, or 8 with a scale for each block and head")
     ap.add_argument("--layers", type=int, default=32)
     ap.add_argument("--other-us", type=float, default=0.0, help="microseconds a token spends in the products with the weights")
     a = ap.parse_args(argv)
     trace = tg.tiny(n_req=max(a.requests, 1))
-    done = measure(trace, a.blocks, batch=a.batch, max_requests=a.requests)
+    done = measure(trace, a.blocks, batch=a.batch, max_requests=a.requests, kept=a.cache)
     t = seconds_per_token(done, a.layers, a.other_us * 1e-6)
     cfgs = tg.configs_for("tiny", trace)
     handle = host.load(trace)
@@ -189,7 +203,7 @@ def main(argv=None):
     flags, n = host.pareto(obj)
     holds = "attention and the cache's upkeep, measured; " + (
         "the products with the weights as given by --other-us" if a.other_us else "without the products with the weights (--other-us)")
-    print(json.dumps({**{k: round(v, 6) for k, v in done.items()}, "layers": a.layers, "other_s_per_token": a.other_us * 1e-6,
+    print(json.dumps({**{k: round(v, 6) for k, v in done.items()}, "cache": a.cache, "layers": a.layers, "other_s_per_token": a.other_us * 1e-6,
                       "t_prefill_per_token": t, "t_prefill_per_token_holds": holds, "configs": int(cfgs.n), "front": int(n)}))
     return done, t, obj, flags
 
