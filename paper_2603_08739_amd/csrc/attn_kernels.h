@@ -515,8 +515,27 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : kKind >= kFp8Blo
     }
     bool look = !kLazy || __any(m == -__builtin_inff());
     for (;;) {
+      if constexpr (kStage) {
+        // Both blocks in turn, their keys read a step ahead.  (Left to the compiler, which has not the
+        // registers to read all of them ahead as in 16 bits, each product waited for its own.)
+        uint4 ahead[2][2];
 #pragma unroll
-      for (int n = 0; n < 2; ++n) {
+        for (int n = 0; n < 2; ++n) {
+          s[n] = f32x16{};
+          ahead[0][n] = lk[L::k_at(32 * n + krow, half)];
+        }
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) {
+          if (d + 1 < D / 16)
+#pragma unroll
+            for (int n = 0; n < 2; ++n) ahead[(d + 1) & 1][n] = lk[L::k_at(32 * n + krow, 2 * (d + 1) + half)];
+#pragma unroll
+          for (int n = 0; n < 2; ++n) s[n] = T::mfma32(ahead[d & 1][n], qf[d], s[n]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < (kStage ? 0 : 2); ++n) {
         s[n] = f32x16{};
         if (kNarrow) {
 #pragma unroll
