@@ -515,7 +515,23 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : kKind >= kFp8Blo
     }
     bool look = !kLazy || __any(m == -__builtin_inff());
     for (;;) {
-      if constexpr (kStage) {
+      if constexpr (kNarrow && kByBlock && D <= 128) {
+        // both blocks in turn, all of their keys read ahead
+        uint4 ahead[2][D / 32];
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+          for (int n = 0; n < 2; ++n) ahead[n][d] = lk[L::k_at(32 * n + krow, 2 * d + half)];
+        __builtin_amdgcn_sched_barrier(0);
+        s[0] = s[1] = f32x16{};
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) {
+#pragma unroll
+          for (int n = 0; n < 2; ++n) s[n] = T::mfma32(widen8<T, kKind>(ahead[n][d].x, ahead[n][d].y), qf[2 * d], s[n]);
+#pragma unroll
+          for (int n = 0; n < 2; ++n) s[n] = T::mfma32(widen8<T, kKind>(ahead[n][d].z, ahead[n][d].w), qf[2 * d + 1], s[n]);
+        }
+      } else if constexpr (kStage) {
         // Both blocks in turn, their keys read a step ahead.  (Left to the compiler, which has not the
         // registers to read all of them ahead as in 16 bits, each product waited for its own.)
         uint4 ahead[2][2];
@@ -535,7 +551,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : kKind >= kFp8Blo
         }
       }
 #pragma unroll
-      for (int n = 0; n < (kStage ? 0 : 2); ++n) {
+      for (int n = 0; n < (kByBlock && D <= 128 ? 0 : 2); ++n) {
         s[n] = f32x16{};
         if (kNarrow) {
 #pragma unroll
