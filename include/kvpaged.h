@@ -219,7 +219,8 @@ typedef struct kv_paged_cache {
  * values are held as value * (1/s) in 32 bits, rounded to nearest even, past +-Q
  * as +-Q; NaN as NaN in e4m3 and 0 as a whole number.  A block is written for one
  * request of a step: requests that share the block a context ends in copy it first,
- * scales too.  Nothing else of the cache is touched. */
+ * scales too.  (Of a request's tokens in one block the first one's slot is looked
+ * at.)  Nothing else of the cache is touched. */
 kv_status kv_paged_append(const kv_paged_batch* b, const kv_paged_cache* c, const kv_rope* rope,
                           uint32_t dtype, kv_heads_view q, kv_heads_view q_out, kv_heads_view k,
                           kv_heads_view v, void* stream);
@@ -249,8 +250,9 @@ kv_status kv_paged_read(const kv_paged_batch* b, const kv_paged_cache* c, uint32
  * lse.  Products are on the matrix cores with 32-bit sums; softmax statistics
  * are in 32 bits; the weights, times the values' scales by block relative to a power
  * of two near the largest, are rounded to the queries' type for the second
- * product (in float16, values in blocks whose scale is below 2^-20 of the largest
- * that a request's queries see lose precision).  Sums are taken with weights of up to 2^14 before the division, so
+ * product, from KV_DT_I8_BLOCK to float16 (there and for float16 queries, values
+ * in blocks whose scale is below 2^-20 of the largest that a request's queries see
+ * lose precision).  Sums are taken with weights of up to 2^14 before the division, so
  * values past some 10^30 may leave the 32-bit range.  Results do not depend on
  * timing.
  *   q, out    views of q_heads heads; out must not overlap q (the

@@ -642,7 +642,7 @@ kv_status paged_read(const kv_paged_batch& b, const kv_paged_cache& c, uint32_t 
   a.kv_heads = b.kv_heads, a.dim_shift = (uint32_t)__builtin_ctz(b.head_dim);
   a.each = (uint32_t)(((uint64_t)b.kv_heads * b.block_size * b.head_dim * bytes + 8191) / 8192);
   const uint64_t tasks = plan_runs(a.runs, row_start, b.n_req, b.block_size, max_rows, max_rows) * 2 * a.each;
-  if (tasks > 0x7fffffffull) return fail(KV_ERR_UNSUPPORTED, "kv_paged_read: too many rows for one call");
+  if (tasks * 64 > 0xffffffffull) return fail(KV_ERR_UNSUPPORTED, "kv_paged_read: too many rows for one call");
   a.tasks = (uint32_t)tasks;
   const uint32_t grid = (uint32_t)((tasks + 3) / 4);
   if (dtype == KV_DT_BF16)

@@ -269,6 +269,52 @@ def test_read(kept, dtype, block, dim, heads):
         assert k2.shape == (part, heads, dim) and torch.equal(k2, k[:part]) and torch.equal(v2, v[:part])
 
 
+@pytest.mark.parametrize("kept", ["i8", "fp8"])
+@pytest.mark.parametrize("block", [16, 32, 64, 128, 256])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_every_block_and_head_size(kept, block, dim):
+    """Parts of blocks, whole blocks and single tokens, written without rotation: numbers are those
+    of 32-bit arithmetic, and come back as such."""
+    import torch
+    from paper_2603_08739_amd import kvpaged as K
+    from tests.paged import blocks_of, held_cache
+    gen = torch.Generator().manual_seed(block + dim)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    J, ctx, new = 3, [0, 5, block - 1, block, 2 * block - 3, 7], [2 * block + 3, block - 5, 1, block, 2, 0]
+    table, n_blocks = blocks_of(ctx, new, block, gen)
+    kc, vc, ks, vs = held_cache(n_blocks, J, block, dim, kept, gen)
+    old = [t.clone() for t in (ks, vs)]
+    total = sum(new)
+    x = (torch.randn(total, 2 * J, dim, generator=gen) * 2).bfloat16().cuda()
+    p = K.Plan(len(ctx), total, block, table.shape[1], J, J, dim)
+    K.kv_paged_plan(p, torch.tensor(ctx, **i32), torch.tensor(new, **i32), table)
+    cache = K.Cache(kc, vc, ks, vs, block_scales=True)
+    K.kv_paged_append(p, cache, x[:, :J], x[:, J:])
+    most = 127.0 if kept == "i8" else 448.0
+    page, at = p.slot // block, p.slot % block
+    for numbers, s, before, want in ((kc, ks, old[0], x[:, :J]), (by_token(vc), vs, old[1], x[:, J:])):
+        top = torch.zeros_like(s).scatter_reduce(0, page[:, None].expand(-1, J), want.float().abs().amax(-1), "amax")
+        need = top / torch.full_like(top, most)
+        begins = torch.zeros(n_blocks, dtype=torch.bool, device="cuda")
+        begins[page[at == 0]] = True
+        touched = torch.zeros_like(begins)
+        touched[page] = True
+        rise = torch.where(need > before, torch.ceil(torch.log2(need.double() / before.double())), 0.0)
+        expect = torch.where(begins[:, None], need, torch.where(touched[:, None], (before.double() * torch.exp2(rise)).float(), before))
+        assert torch.equal(s, expect)
+        y = want.float() * (1.0 / s)[page][:, :, None]
+        y = y.clamp(-most, most)
+        y = y.round() if kept == "i8" else y.to(torch.float8_e4m3fn).float()
+        assert torch.equal(numbers.float()[page, :, at], y)
+    starts, firsts = [0], []
+    for c, n in zip(ctx, new):
+        starts.append(starts[-1] + n)
+        firsts.append(c)
+    k, v = K.kv_paged_read(p, cache, torch.tensor(starts, **i32), first=torch.tensor(firsts, **i32), rows=total)
+    assert torch.equal(k, (kc.float()[page, :, at] * ks[page][:, :, None]).bfloat16())
+    assert torch.equal(v, (vc.float()[page, :, :, at] * vs[page][:, :, None]).bfloat16())
+
+
 def test_read_of_many_requests():
     """Requests by the thousand, ragged and empty ones, rows that do not begin at 0."""
     import torch
