@@ -429,14 +429,21 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : kKind >= kFp8Blo
   // sees has none.  What comes of them goes through LDS a tile ahead, in a place for each
   // wavefront: kept in registers over the products, they would be too many.
   [[maybe_unused]] float k_next = 0.0f, v_next = 0.0f;
+  // groups that some row sees begin at least at `least` and at most at min(key_end - 1, tile_last)
+  [[maybe_unused]] int seen_from = 0;
+  [[maybe_unused]] uint32_t seen_many = 0;
+  if constexpr (kByBlock) {
+    const int least = max(tile_first - window - 14, 0);
+    seen_from = 16 * (lane & 3) - least;
+    seen_many = (uint32_t)max(min(it.key_end - 1, tile_last) - least + 1, 0);
+  }
   [[maybe_unused]] uint32_t unit = 0, unit_now = 0, unit_here = 0;  // the power's exponent bits: of the tile to come, of the present one, of o
   [[maybe_unused]] auto load_scales = [&](int page) {
-    const int64_t from = (int64_t)(there(page) ? page : 0) * a.kv_heads + head;
+    const uint64_t from = (uint64_t)((uint32_t)page < a.n_blocks ? (uint32_t)page : 0u) * a.kv_heads + head;
     k_next = a.k_scale[from], v_next = a.v_scale[from];
   };
   [[maybe_unused]] auto take_scales = [&](int key, int page, int turn) {
-    const int k16 = key + 16 * (lane & 3);
-    const bool seen = there(page) && k16 < it.key_end && k16 <= tile_last && k16 + 15 > tile_first - window;
+    const bool seen = (uint32_t)page < a.n_blocks && (uint32_t)(key + seen_from) < seen_many;
     const float v = seen ? v_next : 0.0f;
     unit = max(unit, (uint32_t)__builtin_amdgcn_readfirstlane((int)(most_of_four(__builtin_bit_cast(uint32_t, v) & 0x7fffffffu) >> 23)));
     const float l2 = __builtin_amdgcn_logf(in_units(v, unit));
@@ -811,7 +818,7 @@ __global__ __launch_bounds__(256, D * NC <= 128 ? 2 : 1) void k_attn_rows(AttnAr
   float k_by = 0.0f, v_by = 0.0f;
   uint32_t unit = 0;
   auto load_scales = [&](int page) {
-    const int64_t from = (int64_t)(there(page) ? page : 0) * a.kv_heads + head;
+    const uint64_t from = (uint64_t)((uint32_t)page < a.n_blocks ? (uint32_t)page : 0u) * a.kv_heads + head;
     k_by = a.k_scale[from], v_by = a.v_scale[from];
   };
   const int first = it.key_begin + kKeys * wave;
