@@ -248,11 +248,11 @@ kv_status kv_paged_read(const kv_paged_batch* b, const kv_paged_cache* c, uint32
  * nothing whatever they hold.  Of what is seen, a score of -inf weighs nothing
  * (no other: as if nothing was seen), one of +inf or NaN leaves NaN in out and
  * lse.  Products are on the matrix cores with 32-bit sums; softmax statistics
- * are in 32 bits; the weights, times the values' scales by block relative to a power
- * of two near the largest, are rounded to the queries' type for the second
- * product, from KV_DT_I8_BLOCK to float16 (there and for float16 queries, values
- * in blocks whose scale is below 2^-20 of the largest that a request's queries see
- * lose precision).  Sums are taken with weights of up to 2^14 before the division, so
+ * are in 32 bits; the weights are rounded to the queries' type for the second
+ * product.  Over a cache with scales by block they are first multiplied by the
+ * values' scales, relative to a power of two near the largest, and rounded to
+ * float16 (so that values in blocks whose scale is below 2^-20 of the largest that
+ * a request's queries see lose precision).  Sums are taken with weights of up to 2^14 before the division, so
  * values past some 10^30 may leave the 32-bit range.  Results do not depend on
  * timing.
  *   q, out    views of q_heads heads; out must not overlap q (the

@@ -28,6 +28,7 @@
 #pragma once
 
 #include <atomic>
+#include <type_traits>
 
 #include "kv_device.h"
 #include "kv_paged.h"
@@ -121,16 +122,14 @@ __device__ __forceinline__ uint4 widen8(uint32_t a, uint32_t b) {
                       T::template widen<true>(b));
 }
 
-// The type of weights and values in the second product: the queries', but for whole
-// numbers float16 whatever that is, which takes fewer instructions to widen them to (8
-// significant bits are exact in both) and rounds weights less.
+// The type of weights and values in the second product: the queries', but with scales by
+// block float16 whatever that is.  Its weights are rounded to 11 bits, not 8 (64 chats of
+// bfloat16: off by 0.0017 of the result, as rounding the result alone is, for 0.0024), and whole numbers
+// take fewer instructions to widen to it; what is held is exact in both, and the
+// scales, which could leave its range, are taken relative to the largest seen.
 template <class T, Kind kKind>
 struct Weights {
-  typedef T type;
-};
-template <class T>
-struct Weights<T, kI8Block> {
-  typedef F16 type;
+  typedef std::conditional_t<(kKind >= kFp8Block), F16, T> type;
 };
 
 struct AttnArgs {
@@ -966,8 +965,8 @@ __global__ __launch_bounds__(256, D * NC <= 128 ? 2 : 1) void k_attn_rows(AttnAr
       for (int e = 0; e < kSteps; ++e) {
         uint4 v = k8 ? e ? widen8<P, kKind>(vf[i].z, vf[i].w) : widen8<P, kKind>(vf[i].x, vf[i].y) : vf[i];
         if (!kFinite && edge) {
-          any |= not_finite<T>(v);
-          v = finite_part<T>(v);
+          any |= not_finite<P>(v);
+          v = finite_part<P>(v);
         }
 #pragma unroll
         for (int n = 0; n < NC; ++n) o[n][i] = P::mfma16(v, p[n][e], o[n][i]);

@@ -15,7 +15,7 @@ def case(ctx, new, block, heads, dim, dtype, kept, window=0, drop=(), max_new=No
     import torch
     from oracle import paged as O
     from paper_2603_08739_amd import kvpaged as K
-    from tests.paged import TYPES, blocks_of, check_attention, held_cache
+    from tests.paged import ROUND, TYPES, blocks_of, check_attention, held_cache
     gen = torch.Generator().manual_seed(seed + 13 * sum(ctx) + sum(new))
     H, J = heads
     table, n_blocks = blocks_of(ctx, new, block, gen)
@@ -47,11 +47,12 @@ def case(ctx, new, block, heads, dim, dtype, kept, window=0, drop=(), max_new=No
     # + the logarithm).  Both together are less than 2^-22 (spread + 8 + reach) of the weight:
     # given to `reach` in units of its own bound, 2 (D + 8) 2^-24 reach.
     want[3] = want[3] + 4 * (spread + 8 + want[3]) / (2 * (dim + 8))
-    if dtype == "f16":
-        # a weight below 2^-14 of the float16 range loses up to 2^-25, with weights of up to 2^6
-        # where 1 is meant: 2^-31 of the largest scale for every key and number
-        most = {"i8": 127.0, "fp8": 448.0}[kept]
-        want[2] = want[2] + 2.0 ** -31 / 2.0 ** -11 * most * float(torch.nan_to_num(vs, nan=0.0, posinf=0.0).max()) * (max(c + n for c, n in zip(ctx, new)) if spread > 12 else 1)
+    # A weight, in float16 whatever the queries' type, that is below its normal numbers loses up to
+    # 2^-25, with weights of 2^6 where 1 is meant: 2^-31 of the largest scale for every key and number
+    # (one key's where the scales are near each other: such weights are small beside the largest).
+    most = {"i8": 127.0, "fp8": 448.0}[kept]
+    keys = max(c + n for c, n in zip(ctx, new)) if spread > 12 else 1
+    want[2] = want[2] + 2.0 ** -31 / ROUND[q.dtype] * most * float(torch.nan_to_num(vs, nan=0.0, posinf=0.0).max()) * keys
     check_attention(out[:total], lse[:total], want, q)
     again = torch.empty_like(out)
     K.kv_paged_attention(p, cache, q, out=again, scale=scale)   # no lse, and bit for bit the same
