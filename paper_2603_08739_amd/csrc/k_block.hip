@@ -11,9 +11,18 @@
 // earlier numbers' roundings add up to less than one unit whatever the number of rises
 // (1/2 + 1/4 + ...), where scales that follow the maximum would add half a unit each time.
 //
-// Both kernels walk over runs: the tokens of one request in one block.  A workgroup
-// takes a run of one head.  No two runs of a step write to one block, so there is
-// no order among workgroups, and no atomics.
+// Both kernels walk over runs: the tokens of one request in one block.  No two runs of a
+// step write to one block, so there is no order among workgroups, and no atomics.
+//
+// Both are bound by memory, and small ones by a chain of round trips (what is known of the
+// request, then its slot or block, then the elements, then the old scale).  Measured, with 32
+// query and 8 key/value heads of 128:
+//   the write of 11,675 prompt tokens (24 requests, blocks of 64, bfloat16 to whole numbers)
+//   85 us from cold caches, 52 in a graph with warm ones; half of it are the queries, 191 MB,
+//   the rest 72 MB; with the read of the blocks it touched 78 us, 340 MB at 4.3 TB/s, where
+//   a large copy does 5.2.  64 single tokens: 4.6 us in a graph of 100, 7 a call (host).
+//   the read of 64 prefixes (135,457 tokens, blocks of 16, heads of 64, 417 MB) 82 us, 5.1 TB/s;
+//   of 4 documents (202,264 tokens, blocks of 64, 1.24 GB) 224 us, 5.5 TB/s.
 #include "rope_device.h"
 
 namespace kv {
@@ -187,7 +196,9 @@ struct BlockArgs {
 };
 
 // A task is a run's keys of one head, or its values: a wavefront for up to 2,048 of
-// a block's numbers, up to 16 of them together.  What goes into the block stays in
+// a block's numbers, up to 16 of them together.  (A workgroup for a run's keys and values that
+// reads them once for the scale and again for the numbers, and turns values byte by byte in LDS,
+// takes 101 us for 85 of the prompts above, from cold caches.)  What goes into the block stays in
 // registers from its largest magnitude to its rounding, so everything is read and written
 // once.
 //   keys     a lane has 16 elements of kItems tokens, turned
