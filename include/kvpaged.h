@@ -194,7 +194,8 @@ typedef struct kv_paged_cache {
                             written by kv_paged_append (memory that may be
                             written, whatever this pointer says); a caller that
                             fills blocks itself gives scales >= 0, 0 for a block
-                            of zeros                                          */
+                            of zeros.  To be written, the two arrays must not be
+                            one                                               */
   const float* v_scale;
 } kv_paged_cache;
 
@@ -226,8 +227,8 @@ kv_status kv_paged_append(const kv_paged_batch* b, const kv_paged_cache* c, cons
                           kv_heads_view v, void* stream);
 
 /* Reads tokens back: row i = row_start[r] .. row_start[r+1] - 1 of request r gets the
- * key and value at position first[r] + i - row_start[r], times its scale, rounded
- * once to dtype (16-bit caches: copied).  Positions that are not in the cache
+ * key and value at position first[r] + i - row_start[r], times its scale in 32 bits,
+ * rounded to dtype (16-bit caches: copied).  Positions that are not in the cache
  * (negative, at or past kv_len, in a block that is not there) give zeros.  Rows past
  * row_start[n_req] are left alone, as are rows past max_rows.
  *   dtype      of k and v: KV_DT_BF16 or KV_DT_F16, a 16-bit cache's own

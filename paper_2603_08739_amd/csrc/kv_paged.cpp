@@ -231,6 +231,8 @@ extern "C" kv_status kv_paged_append(const kv_paged_batch* b, const kv_paged_cac
       if (const char* e = kv::check_view(q)) return invalid(who, e);
       if (const char* e = kv::check_view(q_out)) return invalid(who, e);
     }
+    // (keys and values are written by different workgroups, each with its scale)
+    if (kv::by_block(c->dtype) && c->k_scale == c->v_scale) return invalid(who, "k_scale and v_scale must not be the same");
     if (kv::by_block(c->dtype))
       return kv::paged_append_block(*b, *c, rope ? &rope->table : nullptr, dtype, q, q_out, k, v, (hipStream_t)stream);
     return kv::paged_append(*b, *c, rope ? &rope->table : nullptr, dtype, q, q_out, k, v, (hipStream_t)stream);

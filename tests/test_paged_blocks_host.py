@@ -20,6 +20,14 @@ def test_caches_are_refused(dtype, more, word):
     refused(K, K.LIB.kv_paged_read(ctypes.byref(b), ctypes.byref(c), 0, 0x1000, None, 4, w, w, None), word)
 
 
+@pytest.mark.parametrize("dtype", ["KV_DT_FP8_BLOCK", "KV_DT_I8_BLOCK"])
+def test_one_scale_array_for_both_is_not_written(dtype):
+    from paper_2603_08739_amd import kvpaged as K
+    b, w = batch(K), view(K)
+    c = cache(K, dtype=getattr(K, dtype), k_scale=0x1000, v_scale=0x1000)
+    refused(K, K.LIB.kv_paged_append(ctypes.byref(b), ctypes.byref(c), None, 0, w, w, w, w, None), "same")
+
+
 @pytest.mark.parametrize("kept", [-1, 3, 6, 1 << 31])
 def test_unknown_types_are_refused(kept):
     from paper_2603_08739_amd import kvpaged as K
