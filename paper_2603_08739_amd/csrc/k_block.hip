@@ -18,9 +18,9 @@
 // request, then its slot or block, then the elements, then the old scale).  Measured, with 32
 // query and 8 key/value heads of 128:
 //   the write of 11,675 prompt tokens (24 requests, blocks of 64, bfloat16 to whole numbers)
-//   85 us from cold caches, 52 in a graph with warm ones; half of it are the queries, 191 MB,
-//   the rest 72 MB; with the read of the blocks it touched 78 us, 340 MB at 4.3 TB/s, where
-//   a large copy does 5.2.  64 single tokens: 4.6 us in a graph of 100, 7 a call (host).
+//   81 us from cold caches, 47 in a graph with warm ones; most of it are the queries, 191 MB,
+//   the rest 72 MB (25 us alone); with the read of the blocks it touched 74 us a call, 340 MB at
+//   4.6 TB/s, where a large copy does 5.2.  64 single tokens: 4.6 us in a graph of 100, 7 a call (host).
 //   the read of 64 prefixes (135,457 tokens, blocks of 16, heads of 64, 417 MB) 82 us, 5.1 TB/s;
 //   of 4 documents (202,264 tokens, blocks of 64, 1.24 GB) 224 us, 5.5 TB/s.
 #include "rope_device.h"
@@ -189,16 +189,16 @@ struct BlockArgs {
   float *k_scale, *v_scale;
   uint64_t slots;  // n_blocks * block_size
   uint32_t max_tokens, q_heads, kv_heads, dim_shift, units, rot_dim, heads_each, q_groups;
-  uint32_t q_blocks;  // workgroups of queries; the rest take runs
-  uint32_t waves;     // of a task
-  uint32_t tasks;     // runs by heads by keys or values
+  uint64_t run_share;   // share of workgroups that take runs, in 2^-32; the rest take queries
+  uint32_t waves;       // of a task
+  uint32_t tasks;       // runs by heads by keys or values
   float magnitude;
 };
 
 // A task is a run's keys of one head, or its values: a wavefront for up to 2,048 of
 // a block's numbers, up to 16 of them together.  (A workgroup for a run's keys and values that
 // reads them once for the scale and again for the numbers, and turns values byte by byte in LDS,
-// takes 101 us for 85 of the prompts above, from cold caches.)  What goes into the block stays in
+// takes 101 us for 81 of the prompts above, from cold caches.)  What goes into the block stays in
 // registers from its largest magnitude to its rounding, so everything is read and written
 // once.
 //   keys     a lane has 16 elements of kItems tokens, turned
@@ -207,9 +207,14 @@ struct BlockArgs {
 template <class V, bool kHalf, class H, int kItems>
 __global__ void __launch_bounds__(1024) k_append_block(BlockArgs a) {
   const uint32_t tid = threadIdx.x;
-  if (blockIdx.x < a.q_blocks) {  // queries: as in k_append
+  // Workgroups of runs lie evenly among those of queries: a run is a chain of round trips, and what
+  // queries read and write meanwhile hides it (the prompts above with their read 74 us; queries
+  // first 78, runs first 81).
+  const uint32_t run_block = (uint32_t)((uint64_t)blockIdx.x * a.run_share >> 32);
+  const bool queries = (uint32_t)(((uint64_t)blockIdx.x + 1) * a.run_share >> 32) == run_block;
+  if (queries) {  // as in k_append
     const uint32_t n_tokens = min((uint32_t)max(a.runs.start[a.runs.n_req], 0), a.max_tokens);
-    const uint64_t id = (uint64_t)blockIdx.x * blockDim.x + tid;
+    const uint64_t id = (uint64_t)(blockIdx.x - run_block) * blockDim.x + tid;
     const uint32_t unit = (uint32_t)(id % a.units);
     const uint64_t rest = id / a.units;
     const uint32_t group = (uint32_t)(rest % a.q_groups);
@@ -228,7 +233,7 @@ __global__ void __launch_bounds__(1024) k_append_block(BlockArgs a) {
   // All wavefronts of a task leave together or not at all: there is a barrier below.
   const bool alone = a.waves == 1;
   const uint32_t me = alone ? lane_id() : tid, threads = a.waves * 64;
-  const uint32_t task = alone ? (blockIdx.x - a.q_blocks) * (blockDim.x / 64) + wave_id() : blockIdx.x - a.q_blocks;
+  const uint32_t task = alone ? run_block * (blockDim.x / 64) + wave_id() : run_block;
   if (task >= a.tasks) return;
   const bool keys = !(task & 1);
   const uint32_t place = task / 2 / a.kv_heads, head = task / 2 - place * a.kv_heads;
@@ -626,7 +631,8 @@ kv_status paged_append_block(const kv_paged_batch& b, const kv_paged_cache& c, c
   const uint64_t groups = a.waves == 1 ? (tasks + 3) / 4 : tasks;
   if (tasks > 0x7fffffffull || qs + groups > 0x7fffffffull || (qs + groups) * threads > 0xffffffffull)
     return fail(KV_ERR_UNSUPPORTED, "kv_paged_append: too many heads for one call");
-  a.tasks = (uint32_t)tasks, a.q_blocks = (uint32_t)qs;
+  a.tasks = (uint32_t)tasks;
+  a.run_share = ((groups << 32) + qs + groups - 1) / (qs + groups);  // all of them are `groups` in the end
   const uint32_t grid = (uint32_t)(qs + groups);
   const bool half = !r || r->layout == KV_ROPE_HALF, i8 = c.dtype == KV_DT_I8_BLOCK;
   if (dtype == KV_DT_BF16)
