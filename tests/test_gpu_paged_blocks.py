@@ -416,6 +416,49 @@ def test_a_step_end_to_end_in_a_graph():
         held["ctx"] += 1
 
 
+@pytest.mark.parametrize("dtype, kept", KINDS)
+@pytest.mark.parametrize("window", [0, 20])
+def test_what_a_new_cache_holds_does_not_matter(dtype, kept, window):
+    """Prompts and single tokens over memory that holds anything, scales that are no numbers
+    among it, give what they give over a cleared cache, bit for bit."""
+    import torch
+    from paper_2603_08739_amd import kvpaged as K
+    from tests.paged import TYPES
+    gen = torch.Generator().manual_seed(8)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    R, H, J, D, B, W = 3, 8, 2, 128, 16, 8
+    held = TYPES.get(kept, torch.int8)
+    pool = torch.randperm(R * W + 5, generator=gen).to(torch.int32).cuda()
+    steps = [[33, 5, 60], [1, 1, 1], [0, 30, 1], [1, 1, 1]]
+    inputs = [(torch.randn(sum(n), H + 2 * J, D, generator=gen)).to(TYPES[dtype]).cuda() for n in steps]
+    results = []
+    for dirty in (False, True):
+        kc, vc = torch.zeros(R * W + 5, J, B, D, dtype=torch.int8), torch.zeros(R * W + 5, J, D, B, dtype=torch.int8)
+        ks, vs = torch.zeros(R * W + 5, J), torch.zeros(R * W + 5, J)
+        if dirty:
+            kc, vc = (torch.randint(-128, 128, t.shape, generator=gen).to(torch.int8) for t in (kc, vc))
+            bad = torch.tensor([float("nan"), float("inf"), 1e38, -1.0, 0.0, 1e-42])
+            ks, vs = (bad[torch.randint(0, 6, t.shape, generator=gen)] for t in (ks, vs))
+        cache = K.Cache(*[t.cuda().view(held) for t in (kc, vc)], ks.cuda(), vs.cuda(), block_scales=True)
+        rope = K.Rope(D)
+        table, taken, ctx, outs = torch.full((R, W), -1, **i32), 0, [0] * R, []
+        for new, x in zip(steps, inputs):
+            n = sum(new)
+            p = K.Plan(R, n, B, W, H, J, D, max_new=max(new), window=window)
+            K.kv_paged_plan(p, torch.tensor(ctx, **i32), torch.tensor(new, **i32), table, pool[taken:].contiguous())
+            q = torch.empty(n, H, D, device="cuda", dtype=x.dtype)
+            K.kv_paged_append(p, cache, x[:, H:H + J], x[:, H + J:], q=x[:, :H], q_out=q, rope=rope)
+            outs.append(K.kv_paged_attention(p, cache, q))
+            starts = torch.zeros(R + 1, **i32)
+            starts[1:] = torch.cumsum(p.kv_len, 0)
+            outs += K.kv_paged_read(p, cache, starts, rows=int(starts[-1]), dtype=x.dtype)
+            taken += int(p.result[2])
+            ctx = p.kv_len.tolist()
+        results.append(outs)
+    for a, b in zip(*results):
+        assert bool(torch.isfinite(a.float()).all()) and torch.equal(a.view(torch.int16), b.view(torch.int16))
+
+
 def test_refusals():
     import torch
     from paper_2603_08739_amd import kvpaged as K
