@@ -428,14 +428,18 @@ struct ReadArgs {
 
 // 16-bit caches: numbers are copied
 struct Same {};
-// 8 numbers
-template <int kBytes>
+// so many words
+template <int kWords>
 struct Load {
   typedef uint4 type;
 };
 template <>
-struct Load<1> {
+struct Load<2> {
   typedef uint2 type;
+};
+template <>
+struct Load<1> {
+  typedef uint32_t type;
 };
 
 // 4 numbers, times their scale, in 16 bits
@@ -457,15 +461,16 @@ __device__ __forceinline__ void put_row(uint16_t* p, const uint4& w) {
   __builtin_nontemporal_store(__builtin_bit_cast(u32x4, w), (u32x4*)p);
 }
 
-// A wavefront reads 8 KB of a run's keys, or of its values, whatever heads these are: it
-// shares nothing with others.  Keys go as they lie, 8 elements a load.  Of the values a
-// lane takes 8 elements of as many tokens as 16 bytes hold, turns them in registers
-// and writes 16 bytes of each token's row.
-template <class V, class H>
+// A wavefront reads 2 KB times kWords of a run's keys, or of its values, whatever heads these
+// are: it shares nothing with others.  Keys go as they lie, 8 elements a load.  Of the values
+// a lane takes 8 elements of as many tokens as kWords words hold, turns them in registers
+// and writes 16 bytes of each token's row.  (8 KB, and 2 where that leaves compute units without
+// work: see kFewTasks.)
+template <class V, class H, int kWords>
 __global__ __launch_bounds__(256) void k_read(ReadArgs a) {
   constexpr int kBytes = __is_same(H, Same) ? 2 : 1;
-  constexpr int kTokens = 16 / kBytes;  // of a lane's values
-  constexpr uint32_t kTokenShift = kBytes == 1 ? 4 : 3;
+  constexpr int kTokens = 4 * kWords / kBytes;  // of a lane's values
+  constexpr uint32_t kTokenShift = __builtin_ctz(kTokens);
   const uint32_t lane = lane_id();
   const uint32_t task = blockIdx.x * 4 + wave_id();
   if (task >= a.tasks) return;
@@ -498,9 +503,9 @@ __global__ __launch_bounds__(256) void k_read(ReadArgs a) {
 
   if (keys) {
     const uint8_t* kc = a.kc + page * a.k_block;
-    constexpr int kSteps = 16 / kBytes;  // of 64 lanes by 8 elements
+    constexpr int kSteps = 4 * kWords / kBytes;  // of 64 lanes by 8 elements
     const uint32_t chunk_shift = a.dim_shift - 3;
-    typedef typename Load<kBytes>::type U;
+    typedef typename Load<2 * kBytes>::type U;
     U u[kSteps];
     float by[kSteps];
     auto item = [&](int i, uint32_t& t, uint32_t& head) {
@@ -542,24 +547,30 @@ __global__ __launch_bounds__(256) void k_read(ReadArgs a) {
   const uint32_t t = (item >> chunk_shift << kTokenShift) & ((1u << shift) - 1);
   const uint32_t head = item >> (chunk_shift + shift - kTokenShift);
   if (head >= a.kv_heads || t + kTokens <= begin || t >= end) return;
-  uint4 u[8];
+  typedef typename Load<kWords>::type U;
+  U u[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) u[i] = make_uint4(0, 0, 0, 0);
+  for (int i = 0; i < 8; ++i) u[i] = U{};
   float by = 1.0f;
   if (t < have) {
     by = scale_of(head);
     const uint8_t* p = a.vc + page * a.v_block + (((((int64_t)head << a.dim_shift) + d) << shift) + t) * kBytes;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) u[i] = *(const uint4*)(p + ((int64_t)(i * kBytes) << shift));
+    for (int i = 0; i < 8; ++i) u[i] = *(const U*)(p + ((int64_t)(i * kBytes) << shift));
   }
   uint16_t* out = a.v + (row0 + t) * a.vt + head * a.vh + d;
   auto put = [&](int i, const uint4& w) {
     const uint32_t at = t + i;
     if (at >= begin && at < end) put_row(out + i * a.vt, at < have ? w : make_uint4(0, 0, 0, 0));
   };
-  auto word = [](const uint4& w, int i) { return i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w; };
+  auto word = [](const U& w, int i) {
+    if constexpr (kWords == 1)
+      return w;
+    else
+      return i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w;
+  };
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {  // a word of 4 tokens, or of 2
+  for (int w = 0; w < kWords; ++w) {  // a word of 4 tokens, or of 2
     uint32_t lo[4], hi[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) lo[i] = word(u[i], w), hi[i] = word(u[4 + i], w);
@@ -587,14 +598,25 @@ void launch_append(const BlockArgs& a, bool half, bool more, uint32_t grid, uint
   if (!half && more) hipLaunchKernelGGL((k_append_block<V, false, H, 4>), dim3(grid), dim3(threads), 0, s, a);
 }
 
-template <class V>
-void launch_read(const ReadArgs& a, uint32_t kept, uint32_t grid, hipStream_t s) {
-  if (kept == KV_DT_I8_BLOCK)
-    hipLaunchKernelGGL((k_read<V, I8>), dim3(grid), dim3(256), 0, s, a);
-  else if (eight_bits(kept))
-    hipLaunchKernelGGL((k_read<V, Fp8>), dim3(grid), dim3(256), 0, s, a);
+// Fewer wavefronts than this, two for each SIMD of the chip, leave some without work.
+constexpr uint64_t kFewTasks = 2048;
+
+template <class V, class H>
+void launch_read(const ReadArgs& a, bool few, uint32_t grid, hipStream_t s) {
+  if (few)
+    hipLaunchKernelGGL((k_read<V, H, 1>), dim3(grid), dim3(256), 0, s, a);
   else
-    hipLaunchKernelGGL((k_read<V, Same>), dim3(grid), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_read<V, H, 4>), dim3(grid), dim3(256), 0, s, a);
+}
+
+template <class V>
+void launch_read(const ReadArgs& a, uint32_t kept, bool few, uint32_t grid, hipStream_t s) {
+  if (kept == KV_DT_I8_BLOCK)
+    launch_read<V, I8>(a, few, grid, s);
+  else if (eight_bits(kept))
+    launch_read<V, Fp8>(a, few, grid, s);
+  else
+    launch_read<V, Same>(a, few, grid, s);
 }
 
 }  // namespace
@@ -657,15 +679,19 @@ kv_status paged_read(const kv_paged_batch& b, const kv_paged_cache& c, uint32_t 
   a.by_block = by_block(c.dtype);
   a.max_rows = max_rows, a.max_blocks = b.max_blocks, a.n_blocks = c.n_blocks;
   a.kv_heads = b.kv_heads, a.dim_shift = (uint32_t)__builtin_ctz(b.head_dim);
-  a.each = (uint32_t)(((uint64_t)b.kv_heads * b.block_size * b.head_dim * bytes + 8191) / 8192);
-  const uint64_t tasks = plan_runs(a.runs, row_start, b.n_req, b.block_size, max_rows, max_rows) * 2 * a.each;
+  const uint64_t runs = plan_runs(a.runs, row_start, b.n_req, b.block_size, max_rows, max_rows) * 2;
+  const uint64_t numbers = (uint64_t)b.kv_heads * b.block_size * b.head_dim * bytes;
+  a.each = (uint32_t)((numbers + 8191) / 8192);
+  const bool few = runs * a.each < kFewTasks;
+  if (few) a.each = (uint32_t)((numbers + 2047) / 2048);
+  const uint64_t tasks = runs * a.each;
   if (tasks * 64 > 0xffffffffull) return fail(KV_ERR_UNSUPPORTED, "kv_paged_read: too many rows for one call");
   a.tasks = (uint32_t)tasks;
   const uint32_t grid = (uint32_t)((tasks + 3) / 4);
   if (dtype == KV_DT_BF16)
-    launch_read<bf16x8>(a, c.dtype, grid, s);
+    launch_read<bf16x8>(a, c.dtype, few, grid, s);
   else
-    launch_read<f16x8>(a, c.dtype, grid, s);
+    launch_read<f16x8>(a, c.dtype, few, grid, s);
   KV_HIP(hipGetLastError());
   return KV_OK;
 }
