@@ -443,16 +443,25 @@ struct Load<1> {
   typedef uint32_t type;
 };
 
-// 4 numbers, times their scale, in 16 bits
+// 4 numbers, times their scale, in 16 bits.  A value near the end of float16's range may be held
+// as up to a unit more than it was: what is past the range becomes its largest number, as the
+// write does with its own type's.  (NaN stays NaN.)
 template <class V, class H>
 __device__ __forceinline__ uint2 rows4(uint32_t u, float by) {
   typedef typename Elem<V>::type E;
+  typedef E Pair __attribute__((ext_vector_type(2)));
   float f[4];
   values4<H>(u, f);
-  uint16_t h[4];
+  Pair h[2];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) h[i] = __builtin_bit_cast(uint16_t, (E)(f[i] * by));
-  return make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
+  for (int i = 0; i < 2; ++i) {
+    h[i] = Pair{(E)(f[2 * i] * by), (E)(f[2 * i + 1] * by)};
+    if constexpr (__is_same(V, f16x8)) {
+      const Pair most = {(E)65504.0f, (E)65504.0f};
+      h[i] = __builtin_elementwise_minimum(__builtin_elementwise_maximum(h[i], -most), most);
+    }
+  }
+  return make_uint2(__builtin_bit_cast(uint32_t, h[0]), __builtin_bit_cast(uint32_t, h[1]));
 }
 
 // Rows are written past the caches, which they would fill with what nobody reads twice (64
