@@ -254,7 +254,8 @@ kv_status kv_paged_read(const kv_paged_batch* b, const kv_paged_cache* c, uint32
  * product.  Over a cache with scales by block they are first multiplied by the
  * values' scales, relative to a power of two near the largest, and rounded to
  * float16 (so that values in blocks whose scale is below 2^-20 of the largest that
- * a request's queries see lose precision).  Sums are taken with weights of up to 2^14 before the division, so
+ * a request's queries see lose precision), and float16 results past +-65504, which values near the
+ * end of the range may be held as, are +-65504.  Sums are taken with weights of up to 2^14 before the division, so
  * values past some 10^30 may leave the 32-bit range.  Results do not depend on
  * timing.
  *   q, out    views of q_heads heads; out must not overlap q (the

@@ -132,6 +132,19 @@ struct Weights {
   typedef std::conditional_t<(kKind >= kFp8Block), F16, T> type;
 };
 
+// Two results in the queries' type.  What a cache with scales by block holds may be more than the
+// values that were written, and near the end of float16's range more than it holds: results past
+// the range are its largest number there (NaN stays NaN), not infinities that nobody wrote.
+template <class T, bool kByBlock>
+__device__ __forceinline__ uint32_t pack_result(float a, float b) {
+  const uint32_t u = T::pack(a, b);
+  if constexpr (kByBlock && std::is_same_v<T, F16>) {
+    const f16x2 most = {(_Float16)65504.0f, (_Float16)65504.0f};
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_minimum(__builtin_elementwise_maximum(__builtin_bit_cast(f16x2, u), -most), most));
+  }
+  return u;
+}
+
 struct AttnArgs {
   const uint16_t* q;
   uint16_t* out;
@@ -741,8 +754,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : kKind >= kFp8Blo
   for (int i = 0; i < D / 32; ++i)
 #pragma unroll
     for (int b = 0; b < 4; ++b)
-      *(uint2*)(op + 32 * i + 8 * b + 4 * half) = make_uint2(T::pack(o[i][4 * b] * inv, o[i][4 * b + 1] * inv),
-                                                             T::pack(o[i][4 * b + 2] * inv, o[i][4 * b + 3] * inv));
+      *(uint2*)(op + 32 * i + 8 * b + 4 * half) = make_uint2(pack_result<T, kByBlock>(o[i][4 * b] * inv, o[i][4 * b + 1] * inv),
+                                                             pack_result<T, kByBlock>(o[i][4 * b + 2] * inv, o[i][4 * b + 3] * inv));
   if (a.lse && half == 0)
     a.lse[(int64_t)(it.q_start + token) * a.q_heads + head * G + gh] = (m + __builtin_amdgcn_logf(l)) * kLn2;
   if (mended) add_bad([&](int d, float v) { op[d] = (uint16_t)T::pack(T::value(op[d]) + v, 0.0f); });
@@ -1028,7 +1041,7 @@ __global__ __launch_bounds__(256, D * NC <= 128 ? 2 : 1) void k_attn_rows(AttnAr
     const int token = r / (int)G, gh = r - token * (int)G;
     const float inv = total > 0.0f || total != total ? v_scale / total : 0.0f;
     *(uint2*)(a.out + (int64_t)(it.q_start + token) * a.ot + (int64_t)(head * G + gh) * a.oh + 4 * q) =
-        make_uint2(T::pack(sum[0] * inv, sum[1] * inv), T::pack(sum[2] * inv, sum[3] * inv));
+        make_uint2(pack_result<T, kByBlock>(sum[0] * inv, sum[1] * inv), pack_result<T, kByBlock>(sum[2] * inv, sum[3] * inv));
     if (a.lse && q == 0)
       a.lse[(int64_t)(it.q_start + token) * a.q_heads + head * G + gh] = (top + __builtin_amdgcn_logf(total)) * kLn2;
   };
@@ -1154,7 +1167,7 @@ __global__ __launch_bounds__(256, D * NC <= 128 ? 2 : 1) void k_attn_rows(AttnAr
 // latency: 5 us after the prompt above, 7 after 12 ragged chunks of up to 1,300
 // tokens.  (Joining in the last workgroup of a tile, as with few rows, would leave
 // 128 rows to one workgroup.)
-template <class T>
+template <class T, bool kByBlock>
 __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, uint32_t dim, uint32_t fp8) {
   const uint32_t quads = dim / 4, each = 256 / quads;  // rows of a workgroup
   const uint32_t q = threadIdx.x % quads, chunks = 128 / each;
@@ -1185,7 +1198,7 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a, uint32_t dim, uin
     const float v_scale = fp8 && a.v_scale ? a.v_scale[head] : 1.0f;
     const float inv = total_l > 0.0f || total_l != total_l ? v_scale / total_l : 0.0f;
     *(uint2*)(a.out + (int64_t)(t.q_start + token) * a.ot + (int64_t)(head * a.group + gh) * a.oh + 4 * q) =
-        make_uint2(T::pack(sum[0] * inv, sum[1] * inv), T::pack(sum[2] * inv, sum[3] * inv));
+        make_uint2(pack_result<T, kByBlock>(sum[0] * inv, sum[1] * inv), pack_result<T, kByBlock>(sum[2] * inv, sum[3] * inv));
     if (a.lse && q == 0)
       a.lse[(int64_t)(t.q_start + token) * a.q_heads + head * a.group + gh] =
           (top + __builtin_amdgcn_logf(total_l)) * kLn2;

@@ -61,9 +61,11 @@ kv_status paged_attention(const kv_paged_batch& b, const WorkLayout& w, const kv
   const bool by_head = c.dtype == KV_DT_FP8;
   const dim3 join(std::min<uint32_t>(w.max_split * b.kv_heads * 4, 4096));
   if (dtype == KV_DT_BF16)
-    hipLaunchKernelGGL(k_attn_join<BF16>, join, dim3(256), 0, s, a, b.head_dim, (uint32_t)by_head);
+    hipLaunchKernelGGL((k_attn_join<BF16, false>), join, dim3(256), 0, s, a, b.head_dim, (uint32_t)by_head);
+  else if (by_block(c.dtype))
+    hipLaunchKernelGGL((k_attn_join<F16, true>), join, dim3(256), 0, s, a, b.head_dim, 0u);
   else
-    hipLaunchKernelGGL(k_attn_join<F16>, join, dim3(256), 0, s, a, b.head_dim, (uint32_t)by_head);
+    hipLaunchKernelGGL((k_attn_join<F16, false>), join, dim3(256), 0, s, a, b.head_dim, (uint32_t)by_head);
   KV_HIP(hipGetLastError());
   return KV_OK;
 }
