@@ -194,8 +194,8 @@ typedef struct kv_paged_cache {
                             written by kv_paged_append (memory that may be
                             written, whatever this pointer says); a caller that
                             fills blocks itself gives scales >= 0, 0 for a block
-                            of zeros.  To be written, the two arrays must not be
-                            one                                               */
+                            of zeros.  To be written, the two arrays must not
+                            overlap                                           */
   const float* v_scale;
 } kv_paged_cache;
 

@@ -222,6 +222,11 @@ extern "C" kv_status kv_paged_append(const kv_paged_batch* b, const kv_paged_cac
     if (!b || !c) return invalid(who, "batch or cache is NULL");
     if (const char* e = kv::check_batch(*b)) return invalid(who, e);
     if (const char* e = kv::check_cache(*c, *b, dtype)) return invalid(who, e);
+    if (kv::by_block(c->dtype)) {  // keys and values are written by different workgroups, each with its scale
+      const uintptr_t ks = (uintptr_t)c->k_scale, vs = (uintptr_t)c->v_scale;
+      if ((ks > vs ? ks - vs : vs - ks) < (uint64_t)c->n_blocks * b->kv_heads * sizeof(float))
+        return invalid(who, "k_scale and v_scale must not be the same or overlap");
+    }
     if (rope && !kv::rope_is_live(rope)) return invalid(who, "not a live rotation");
     if (rope && rope->table.rot_dim > b->head_dim) return invalid(who, "the rotation is wider than a head");
     if (rope && kv::rope_is_elsewhere(rope)) return invalid(who, "the rotation is on another device");
@@ -231,8 +236,6 @@ extern "C" kv_status kv_paged_append(const kv_paged_batch* b, const kv_paged_cac
       if (const char* e = kv::check_view(q)) return invalid(who, e);
       if (const char* e = kv::check_view(q_out)) return invalid(who, e);
     }
-    // (keys and values are written by different workgroups, each with its scale)
-    if (kv::by_block(c->dtype) && c->k_scale == c->v_scale) return invalid(who, "k_scale and v_scale must not be the same");
     if (kv::by_block(c->dtype))
       return kv::paged_append_block(*b, *c, rope ? &rope->table : nullptr, dtype, q, q_out, k, v, (hipStream_t)stream);
     return kv::paged_append(*b, *c, rope ? &rope->table : nullptr, dtype, q, q_out, k, v, (hipStream_t)stream);
