@@ -367,6 +367,8 @@ def kv_paged_read(plan: Plan, cache: Cache, row_start, first=None, k=None, v=Non
     heads, _, dim = cache.shape
     if (k is None) != (v is None):
         raise ValueError("k and v go together")
+    if rows is not None and rows < 0:  # (the library would take its lowest 32 bits)
+        raise ValueError(f"rows is {rows}; expected none or more")
     if k is None:
         if rows is None:
             raise ValueError("either k and v or the number of rows has to be given")
