@@ -232,9 +232,9 @@ __device__ __forceinline__ float element(const uint8_t* p) {
 //
 // One prompt of 8,111 tokens after 256 cached ones, 32 query and 8 key/value heads of
 // 128, bf16: 573 GFLOP over the keys that queries see in 557 to 619 us (cards
-// differ), 0.93 to 1.03 PFLOP/s where a large matrix product does 1.3 to 1.4; on a card
-// that has rested before each call 630, under a kernel trace up to 690.  The matrix
-// cores are busy half of the time: the exponentials, conversions and masks take
+// differ), 0.93 to 1.03 PFLOP/s where a large matrix product does 1.15 to 1.35 (8,192
+// and 16,384 squared on one card); on a card that has rested before each call 630,
+// under a kernel trace up to 690.  The matrix cores are busy half of the time: the exponentials, conversions and masks take
 // vector instructions, of which two wavefronts on a SIMD hide a part only.  The same
 // prompt over an 8-bit cache: 579 us beside 571.  Heads of 64: 885 TFLOP/s, 8 bits the
 // same; half of the products for each exponential.  Heads of 256: 685, 8 bits 770; one
@@ -244,11 +244,13 @@ __device__ __forceinline__ float element(const uint8_t* p) {
 // wavefront priorities (the same).
 //
 // With scales by block, 7,777 tokens after 300, 32 query and 8 key/value heads of 128, bfloat16
-// over whole numbers: 534 GFLOP in 586 to 605 us, 0.88 to 0.91 PFLOP/s; 5,003 after 2,000,
-// float16 over e4m3 in blocks of 64: 369 GFLOP in 404 to 419 us, 0.88 to 0.91.  Beside e4m3
-// with scales by head 7 and 5 % longer (heads of 64: 15 and 12).  A wavefront's tile takes 300
-// vector instructions beside its 32 products, 27 of them for the scales; whole numbers 270, of
-// which 80 widen its share; 16 bits 150.  The matrix cores are busy 42 % of the time (16 bits 49).
+// over whole numbers: 534 GFLOP in 581 to 605 us, 0.88 to 0.92 PFLOP/s; 5,003 after 2,000,
+// float16 over e4m3 in blocks of 64: 369 GFLOP in 404 to 421 us, 0.88 to 0.91.  In turn on one
+// card, calls that follow one another, the first prompt over e4m3 with scales by head takes 528
+// us, by block 563, whole numbers 581 (heads of 64: 304, 348, 354; 16 and 4 heads of 256: 707, 742,
+// 948).  A wavefront's tile takes 300 vector instructions beside its 32 products, 27 of them for
+// the scales; whole numbers 270, of which 80 widen its share; 16 bits 150.  The matrix cores are
+// busy 42 % of the time (16 bits 49).
 template <int D, int kBytes>
 struct TileLds {
   static constexpr int kRowChunks = D * kBytes / 16;              // of a row of K
@@ -296,7 +298,10 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : kKind >= kFp8Blo
   constexpr bool k8 = kKind != kSixteen, kByBlock = kKind >= kFp8Block;
   constexpr bool kFinite = kKind == kI8Block;  // nothing held is anything else
   typedef typename Weights<T, kKind>::type P;
-  constexpr bool kStage = kKind == kI8Block && D <= 128;  // widened on the way into LDS
+  // Whole numbers are widened on the way into LDS.  Heads of 256 have no registers for numbers that
+  // wait for it (256 and 204 are in use): every wavefront widens all of a tile, which is what they
+  // take beyond e4m3 (948 us for 742, see above).
+  constexpr bool kStage = kKind == kI8Block && D <= 128;
   constexpr bool kNarrow = k8 && !kStage;                 // 8 bits in LDS
   constexpr int BK = 64, kBytes = k8 ? 1 : 2;
   typedef TileLds<D, kNarrow ? 1 : 2> L;
@@ -383,7 +388,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 128 ? 2 : kKind >= kFp8Blo
   };
   // Whole numbers take two or three instructions for two to widen, and every wavefront reads all
   // of the tile: they are widened once, by the one that has loaded them.  (With loads of 8 bytes
-  // its writes to LDS would not meet on banks, but the prompt took 860 us for 830.)
+  // its writes to LDS would not meet on banks, but the prompt took 860 us for the 830 that it did
+  // before this ran beside the products.)
   [[maybe_unused]] auto put = [&](uint4* lk, uint4* lv) {
     constexpr int kRow = D / 16;  // chunks of 16 numbers of a key
 #pragma unroll

@@ -21,9 +21,11 @@
 //   81 us from cold caches, 47 in a graph with warm ones; most of it are the queries, 191 MB,
 //   the rest 72 MB (25 us alone); with the read of the blocks it touched 74 us a call, 340 MB at
 //   4.6 TB/s, where a large copy does 5.2.  64 single tokens: 4.6 us in a graph of 100, 7 a call (host).
+//   1,000 single tokens, keys and values of 8 heads: 17.7 us in a graph in blocks of 16, 48 in blocks of 64
+//   (into 16-bit caches 12.7 and 15.1): a task has wavefronts for all of its block, whatever goes into it.
 //   the read of 64 prefixes (135,457 tokens, blocks of 16, heads of 64, 417 MB) 82 us, 5.1 TB/s;
-//   of 4 documents (202,264 tokens, blocks of 64, 1.24 GB) 224 us, 5.5 TB/s; of 3 chats (155
-//   tokens) 3.6 us in a graph, 7 a call (host).
+//   of 4 documents (202,264 tokens, blocks of 64, 1.24 GB) 225 us, 5.5 TB/s; of 3 chats (155
+//   tokens) 3.5 us in a graph, 7 a call (host).
 #include "rope_device.h"
 
 namespace kv {
@@ -464,8 +466,8 @@ __device__ __forceinline__ uint2 rows4(uint32_t u, float by) {
   return make_uint2(__builtin_bit_cast(uint32_t, h[0]), __builtin_bit_cast(uint32_t, h[1]));
 }
 
-// Rows are written past the caches, which they would fill with what nobody reads twice (64
-// prefixes, 417 MB read and written: 67 us, with plain stores 93).
+// Rows are written past the caches, which they would fill with what nobody reads twice (the
+// prefixes above 82 us, with plain stores 88; the documents 225 and 243).
 __device__ __forceinline__ void put_row(uint16_t* p, const uint4& w) {
   typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
   __builtin_nontemporal_store(__builtin_bit_cast(u32x4, w), (u32x4*)p);
@@ -474,9 +476,9 @@ __device__ __forceinline__ void put_row(uint16_t* p, const uint4& w) {
 // A wavefront reads 2 KB times kWords of a run's keys, or of its values, whatever heads these
 // are: it shares nothing with others.  Keys go as they lie, 8 elements a load.  Of the values
 // a lane takes 8 elements of as many tokens as kWords words hold, turns them in registers
-// and writes 16 bytes of each token's row.  8 KB (the documents above 226 us, with 2 KB 274; blocks
-// of 16 the same with both), and 2 where that leaves compute units without work (the chats 3.6
-// us, with 8 KB 6.9): see kFewTasks.
+// and writes 16 bytes of each token's row.  8 KB (the documents above 225 us, with 2 KB 273; blocks
+// of 16 the same with both), and 2 where that leaves compute units without work (the chats 3.5
+// us in a graph, with 8 KB 6.9): see kFewTasks.
 template <class V, class H, int kWords>
 __global__ __launch_bounds__(256) void k_read(ReadArgs a) {
   constexpr int kBytes = __is_same(H, Same) ? 2 : 1;
