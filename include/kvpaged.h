@@ -228,8 +228,8 @@ kv_status kv_paged_append(const kv_paged_batch* b, const kv_paged_cache* c, cons
 
 /* Reads tokens back: row i = row_start[r] .. row_start[r+1] - 1 of request r gets the
  * key and value at position first[r] + i - row_start[r], times its scale in 32 bits,
- * rounded to dtype (16-bit caches: copied); in float16 what is past +-65504, which a value
- * near the end of the range may be held as, is +-65504.  Positions that are not in the cache
+ * rounded to dtype (16-bit caches: copied); what is past dtype's range, as a value near its
+ * end may be held, is its largest number.  Positions that are not in the cache
  * (negative, at or past kv_len, in a block that is not there) give zeros.  Rows past
  * row_start[n_req] are left alone, as are rows past max_rows.
  *   dtype      of k and v: KV_DT_BF16 or KV_DT_F16, a 16-bit cache's own

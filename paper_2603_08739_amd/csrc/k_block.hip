@@ -18,14 +18,14 @@
 // request, then its slot or block, then the elements, then the old scale).  Measured, with 32
 // query and 8 key/value heads of 128:
 //   the write of 11,675 prompt tokens (24 requests, blocks of 64, bfloat16 to whole numbers)
-//   81 us from cold caches, 47 in a graph with warm ones; most of it are the queries, 191 MB,
+//   81 us from cold caches, 48 in a graph with warm ones; most of it are the queries, 191 MB,
 //   the rest 72 MB (25 us alone); with the read of the blocks it touched 74 us a call, 340 MB at
-//   4.6 TB/s, where a large copy does 5.2.  64 single tokens: 4.6 us in a graph of 100, 7 a call (host).
+//   4.6 TB/s, where a large copy does 5.2.  64 single tokens: 5.1 us in a graph of 100, 7 a call (host).
 //   1,000 single tokens, keys and values of 8 heads: 17.7 us in a graph in blocks of 16, 48 in blocks of 64
 //   (into 16-bit caches 12.7 and 15.1): a task has wavefronts for all of its block, whatever goes into it.
-//   the read of 64 prefixes (135,457 tokens, blocks of 16, heads of 64, 417 MB) 82 us, 5.1 TB/s;
-//   of 4 documents (202,264 tokens, blocks of 64, 1.24 GB) 225 us, 5.5 TB/s; of 3 chats (155
-//   tokens) 3.5 us in a graph, 7 a call (host).
+//   the read of 64 prefixes (135,457 tokens, blocks of 16, heads of 64, 417 MB) 80 us, 5.2 TB/s;
+//   of 4 documents (202,264 tokens, blocks of 64, 1.24 GB) 219 us, 5.7 TB/s; of 3 chats (155
+//   tokens) 3.6 us in a graph, 7 a call (host).
 #include "rope_device.h"
 
 namespace kv {
@@ -445,29 +445,33 @@ struct Load<1> {
   typedef uint32_t type;
 };
 
-// 4 numbers, times their scale, in 16 bits.  A value near the end of float16's range may be held
+// 4 numbers, times their scale, in 16 bits.  A value near the end of the type's range may be held
 // as up to a unit more than it was: what is past the range becomes its largest number, as the
-// write does with its own type's.  (NaN stays NaN.)
+// write does with its own type's.  (NaN stays NaN.)  `past`: whether some scale of the wavefront's
+// can bring that about (asked of every number, the documents above take 227 us for 219).
 template <class V, class H>
-__device__ __forceinline__ uint2 rows4(uint32_t u, float by) {
+__device__ __forceinline__ uint2 rows4(uint32_t u, float by, bool past) {
   typedef typename Elem<V>::type E;
-  typedef E Pair __attribute__((ext_vector_type(2)));
+  constexpr float kMost = Elem<V>::kMost;
   float f[4];
   values4<H>(u, f);
-  Pair h[2];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    h[i] = Pair{(E)(f[2 * i] * by), (E)(f[2 * i + 1] * by)};
-    if constexpr (__is_same(V, f16x8)) {
-      const Pair most = {(E)65504.0f, (E)65504.0f};
-      h[i] = __builtin_elementwise_minimum(__builtin_elementwise_maximum(h[i], -most), most);
-    }
-  }
-  return make_uint2(__builtin_bit_cast(uint32_t, h[0]), __builtin_bit_cast(uint32_t, h[1]));
+  for (int i = 0; i < 4; ++i) f[i] *= by;
+  if (past)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = __builtin_elementwise_minimum(__builtin_elementwise_maximum(f[i], -kMost), kMost);
+  uint16_t h[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) h[i] = __builtin_bit_cast(uint16_t, (E)f[i]);
+  return make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
+}
+template <class V, class H>
+__device__ __forceinline__ bool may_pass(float by) {  // (whole numbers that a caller filled in may be -128)
+  return fabsf(by) > Elem<V>::kMost / (H::kMost + 1.0f);
 }
 
 // Rows are written past the caches, which they would fill with what nobody reads twice (the
-// prefixes above 82 us, with plain stores 88; the documents 225 and 243).
+// prefixes above 80 us, with plain stores 86; the documents 219 and 239).
 __device__ __forceinline__ void put_row(uint16_t* p, const uint4& w) {
   typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
   __builtin_nontemporal_store(__builtin_bit_cast(u32x4, w), (u32x4*)p);
@@ -476,9 +480,9 @@ __device__ __forceinline__ void put_row(uint16_t* p, const uint4& w) {
 // A wavefront reads 2 KB times kWords of a run's keys, or of its values, whatever heads these
 // are: it shares nothing with others.  Keys go as they lie, 8 elements a load.  Of the values
 // a lane takes 8 elements of as many tokens as kWords words hold, turns them in registers
-// and writes 16 bytes of each token's row.  8 KB (the documents above 225 us, with 2 KB 273; blocks
-// of 16 the same with both), and 2 where that leaves compute units without work (the chats 3.5
-// us in a graph, with 8 KB 6.9): see kFewTasks.
+// and writes 16 bytes of each token's row.  8 KB (the documents above 219 us, with 2 KB 273; the
+// prefixes 80 and 81), and 2 where that leaves compute units without work (the chats 3.6 us in a
+// graph, with 8 KB 6.3): see kFewTasks.
 template <class V, class H, int kWords>
 __global__ __launch_bounds__(256) void k_read(ReadArgs a) {
   constexpr int kBytes = __is_same(H, Same) ? 2 : 1;
@@ -537,6 +541,12 @@ __global__ __launch_bounds__(256) void k_read(ReadArgs a) {
         by[i] = scale_of(head);
       }
     }
+    bool past = false;
+    if constexpr (kBytes == 1) {
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) past |= may_pass<V, H>(by[i]);
+      past = __any(past);
+    }
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
       uint32_t t, head;
@@ -544,7 +554,7 @@ __global__ __launch_bounds__(256) void k_read(ReadArgs a) {
       if (head >= a.kv_heads || t < begin || t >= end) continue;
       uint4 w;
       if constexpr (kBytes == 1) {
-        const uint2 lo = rows4<V, H>(u[i].x, by[i]), hi = rows4<V, H>(u[i].y, by[i]);
+        const uint2 lo = rows4<V, H>(u[i].x, by[i], past), hi = rows4<V, H>(u[i].y, by[i], past);
         w = make_uint4(lo.x, lo.y, hi.x, hi.y);
       } else {
         w = u[i];
@@ -571,6 +581,8 @@ __global__ __launch_bounds__(256) void k_read(ReadArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) u[i] = *(const U*)(p + ((int64_t)(i * kBytes) << shift));
   }
+  bool past = false;
+  if constexpr (kBytes == 1) past = __any(may_pass<V, H>(by));
   uint16_t* out = a.v + (row0 + t) * a.vt + head * a.vh + d;
   auto put = [&](int i, const uint4& w) {
     const uint32_t at = t + i;
@@ -592,7 +604,7 @@ __global__ __launch_bounds__(256) void k_read(ReadArgs a) {
       turn_bytes(hi);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const uint2 x = rows4<V, H>(lo[i], by), y = rows4<V, H>(hi[i], by);
+        const uint2 x = rows4<V, H>(lo[i], by, past), y = rows4<V, H>(hi[i], by, past);
         put(4 * w + i, make_uint4(x.x, x.y, y.x, y.y));
       }
     } else {

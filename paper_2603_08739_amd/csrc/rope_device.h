@@ -15,10 +15,12 @@ struct Elem;
 template <>
 struct Elem<bf16x8> {
   typedef __bf16 type;
+  static constexpr float kMost = 0x1.fep127f;  // the largest number
 };
 template <>
 struct Elem<f16x8> {
   typedef _Float16 type;
+  static constexpr float kMost = 65504.0f;
 };
 
 template <class V>

@@ -360,8 +360,8 @@ def kv_paged_read(plan: Plan, cache: Cache, row_start, first=None, k=None, v=Non
     as rows row_start[r] .. row_start[r+1] - 1 (int32 [n_req+1]) of k and v: [rows,
     kv_heads, dim] bfloat16 / float16.  k and v go together; where they are None they are
     made, with `rows` rows (rows that nothing is read into hold anything) of `dtype`,
-    the cache's own or bfloat16.  float16 rows of a cache of 8 bits end at +-65504.
-    Returns (k, v)."""
+    the cache's own or bfloat16.  Rows of a cache of 8 bits end at dtype's largest
+    number.  Returns (k, v)."""
     dev = _device()
     b, _ = _fits(plan, cache, dev)
     heads, _, dim = cache.shape

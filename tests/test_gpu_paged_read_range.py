@@ -90,3 +90,44 @@ def test_the_ends_of_the_range(kept, blocks):
             assert torch.equal(torch.isnan(got), torch.isnan(want)) and bool(torch.isnan(want).any()) == (kept != "i8")
             number = ~torch.isnan(want)
             assert torch.equal(got[number], want[number].to(dtype))
+
+
+# In units of 2^120, bfloat16's largest number is 255.  A first token of 254, then one of 255: the scale is doubled to 4, and 255
+# is held as 64 units, 2^128.  In e4m3, after 240: 238 units, held as 240, 257 x 2^120.
+@pytest.mark.parametrize("kept, before, held", [("i8", 254.0, 64.0), ("fp8", 240.0, 240.0)])
+def test_finite_values_come_back_finite_in_bfloat16(kept, before, held):
+    import torch
+    from paper_2603_08739_amd import kvpaged as K
+    i32 = dict(dtype=torch.int32, device="cuda")
+    kind, most = torch.int8 if kept == "i8" else torch.float8_e4m3fn, 255.0 * 2.0 ** 120
+    kc, vc = torch.zeros(1, 1, 16, 64, device="cuda", dtype=kind), torch.zeros(1, 1, 64, 16, device="cuda", dtype=kind)
+    cache = K.Cache(kc, vc, torch.zeros(1, 1, device="cuda"), torch.zeros(1, 1, device="cuda"), block_scales=True)
+    table = torch.zeros(1, 1, **i32)
+    p = K.Plan(1, 1, 16, 1, 1, 1, 64, max_new=1)
+    for t, size in enumerate((before * 2.0 ** 120, most)):
+        x = torch.zeros(1, 2, 64, device="cuda", dtype=torch.bfloat16)
+        x[0, :, 3], x[0, :, 5] = size, -size
+        K.kv_paged_plan(p, torch.tensor([t], **i32), torch.ones(1, **i32), table)
+        K.kv_paged_append(p, cache, x[:, :1], x[:, 1:])
+    assert kc[0, 0, 1, 3].float() == held and vc[0, 0, 5, 1].float() == -held
+    # the last step's plan, one token in the cache and one new
+    for got in K.kv_paged_read(p, cache, torch.tensor([0, 2], **i32), rows=2):
+        assert got[1, 0, 3] == most and got[1, 0, 5] == -most and not got[1, 0, 6]
+        assert bool(torch.isfinite(got).all())
+
+
+def test_nan_and_large_scales_by_head_in_bfloat16():
+    import torch
+    from paper_2603_08739_amd import kvpaged as K
+    i32 = dict(dtype=torch.int32, device="cuda")
+    codes = torch.arange(-128, 128, dtype=torch.int32).to(torch.int8).reshape(1, 1, 16, 16).repeat(1, 2, 1, 4).cuda()  # every e4m3 number
+    kc, vc = codes.view(torch.float8_e4m3fn), codes.transpose(2, 3).contiguous().view(torch.float8_e4m3fn)
+    scale = torch.tensor([1.0, 2.0 ** 121], device="cuda")
+    p = K.Plan(1, 1, 16, 1, 2, 2, 64)
+    K.kv_paged_plan(p, torch.tensor([16], **i32), torch.zeros(1, **i32), torch.zeros(1, 1, **i32))
+    k, v = K.kv_paged_read(p, K.Cache(kc, vc, scale, scale), torch.tensor([0, 16], **i32), rows=16)
+    want = (kc[0].float() * scale[:, None, None]).clamp(-255.0 * 2.0 ** 120, 255.0 * 2.0 ** 120).bfloat16().transpose(0, 1)
+    for got in (k, v):
+        assert torch.equal(torch.isnan(got), torch.isnan(want)) and int(torch.isnan(got).sum()) == 2 * 2 * 4
+        number = ~torch.isnan(want)
+        assert torch.equal(got[number], want[number])
