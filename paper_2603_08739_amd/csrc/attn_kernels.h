@@ -234,9 +234,10 @@ __device__ __forceinline__ float element(const uint8_t* p) {
 // 128, bf16: 573 GFLOP over the keys that queries see in 557 to 619 us (cards
 // differ), 0.93 to 1.03 PFLOP/s where a large matrix product does 1.15 to 1.35 (8,192
 // and 16,384 squared on one card); on a card that has rested before each call 630,
-// under a kernel trace up to 690.  The matrix cores are busy half of the time: the exponentials, conversions and masks take
-// vector instructions, of which two wavefronts on a SIMD hide a part only.  The same
-// prompt over an 8-bit cache: 579 us beside 571.  Heads of 64: 885 TFLOP/s, 8 bits the
+// under a kernel trace up to 690.  The matrix cores are busy half of the time: the
+// exponentials, conversions and masks take vector instructions, of which two
+// wavefronts on a SIMD hide a part only.  The same prompt over an 8-bit cache: 579 us
+// beside 571.  Heads of 64: 885 TFLOP/s, 8 bits the
 // same; half of the products for each exponential.  Heads of 256: 685, 8 bits 770; one
 // wavefront on a SIMD has the registers, so that nothing hides its softmax.  What was
 // tried beside it and was no faster: the next scores worked out between the steps of
