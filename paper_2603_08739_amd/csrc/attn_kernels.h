@@ -245,8 +245,8 @@ __device__ __forceinline__ float element(const uint8_t* p) {
 // wavefront priorities (the same).
 //
 // With scales by block, 7,777 tokens after 300, 32 query and 8 key/value heads of 128, bfloat16
-// over whole numbers: 534 GFLOP in 581 to 605 us, 0.88 to 0.92 PFLOP/s; 5,003 after 2,000,
-// float16 over e4m3 in blocks of 64: 369 GFLOP in 404 to 421 us, 0.88 to 0.91.  In turn on one
+// over whole numbers: 534 GFLOP in 581 to 620 us, 0.86 to 0.92 PFLOP/s; 5,003 after 2,000,
+// float16 over e4m3 in blocks of 64: 369 GFLOP in 404 to 424 us, 0.87 to 0.91.  In turn on one
 // card, calls that follow one another, the first prompt over e4m3 with scales by head takes 528
 // us, by block 563, whole numbers 581 (heads of 64: 304, 348, 354; 16 and 4 heads of 256: 707, 742,
 // 948).  A wavefront's tile takes 300 vector instructions beside its 32 products, 27 of them for
